@@ -85,8 +85,9 @@ def draw(rng):
         B //= 2
     ragged = B > 1 and rng.random() < 0.6
     new = _log_int(rng, 1, 25600) if kind == "write" else 0
-    if kind == "write" and B * H * new * d > 8e8:
-        new = int(8e8 / (B * H * d))
+    most = 8e8 if dtype == "bf16" else 4.8e8
+    if kind == "write" and B * H * new * d > most:
+        new = int(most / (B * H * d))
     if kind == "write" and (not ragged or rng.random() < 0.5):
         length = rng.choice([0, length])
     cap = -(-(length + max(new, 1) + rng.randrange(300)) // block) * block
