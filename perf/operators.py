@@ -81,7 +81,7 @@ def draw(rng):
     H, G = rng.choice([(2, 2), (4, 7), (8, 4), (8, 4), (8, 8), (32, 1), (5, 3)])
     B = rng.choice([1, 1, 2, 5, 16, 32])
     length = _log_int(rng, 1, 102400)
-    while B > 1 and B * H * length * d > 6e8:
+    while B > 1 and B * H * length * d > (6e8 if dtype == "bf16" else 4.5e8):
         B //= 2
     ragged = B > 1 and rng.random() < 0.6
     new = _log_int(rng, 1, 25600) if kind == "write" else 0
