@@ -376,6 +376,126 @@ SELKV_API selkv_status selkv_decode_append(const selkv_params* p, const void* q,
                                            int32_t capacity, float* out, void* ws, size_t ws_bytes,
                                            hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * The cache in 8 bits
+ *
+ * A cache (compressed or not) that is kept as 8-bit codes with one scale for
+ * each block of tokens of a KV head, decoded over without being expanded.
+ *
+ * Quantisation.  Entries are grouped into blocks of T = selkv_cache8.block
+ * tokens of one KV head; K and V each have their own scale.  With a the
+ * largest magnitude of the block's T*d finite elements and top = 127 (int8)
+ * or 448 (e4m3):
+ *   scale = a / top,  code = round-to-nearest-even(x * (top / a)),  value = code * scale,
+ * the divisions and the product in fp32.  A block with a < 2^-100 is stored
+ * as zeros with scale 0.  An infinite element gets the code +-top, a NaN the
+ * code 0: neither changes what its neighbours are stored as.
+ *
+ * The open block.  Only whole blocks are quantised, each once, when its last
+ * row arrives.  The rows of the last, incomplete block stay in the storage
+ * type in a tail of T rows per KV head: entry e waits in row e mod T.  So a
+ * cache written in any number of pieces holds bit for bit the codes and
+ * scales that one write gives, and no code is ever rounded twice.
+ *
+ * Lengths.  Every call takes `cache_len` and `lens`.  lens = NULL: every
+ * sequence holds cache_len entries.  Otherwise lens[b] (int32, on the device)
+ * is the number of entries of sequence b and cache_len an upper bound of them
+ * that the host knows; the library only reads lens (the caller advances it
+ * after a call that appends), so a captured call follows it from replay to
+ * replay.  A negative lens[b] marks a sequence that takes no part: nothing of
+ * it is stored, and its decode outputs are 0.  A lens[b] above cache_len is
+ * taken as cache_len.
+ * ------------------------------------------------------------------------- */
+
+typedef enum selkv_code8 {
+  SELKV_I8 = 0,    /* signed integers, -127 .. 127 */
+  SELKV_E4M3 = 1   /* OCP fp8 e4m3 (largest value 448) */
+} selkv_code8;
+
+/* An 8-bit cache: its sizes and the caller's device buffers.  H_kv, d, the
+ * number of sequences B and the storage type come from selkv_params. */
+typedef struct selkv_cache8 {
+  uint32_t struct_size;  /* = sizeof(selkv_cache8) */
+  int32_t code;          /* selkv_code8 */
+  int32_t block;         /* T: tokens per scale, 16, 32, 64 or 128 (default 64) */
+  int32_t capacity;      /* entries per KV head that the buffers hold: a multiple of T, at most 2^28 */
+  void* K;               /* codes [B, H_kv, capacity, d] */
+  void* V;               /* codes [B, H_kv, capacity/16, d, 16]: the 16 tokens of a tile side by side per channel */
+  float* k_scale;        /* [B, H_kv, capacity/T] */
+  float* v_scale;        /* [B, H_kv, capacity/T] */
+  void* k_tail;          /* [B, H_kv, T, d] in kv_dtype: rows of the open block */
+  void* v_tail;          /* [B, H_kv, T, d] in kv_dtype */
+} selkv_cache8;
+
+/* Fill `c` with the defaults: int8, T = 64, capacity 0 and NULL pointers (to
+ * be set).  The buffers themselves need no initialisation. */
+SELKV_API void selkv_cache8_init(selkv_cache8* c);
+
+/* Append rows to every sequence: entries lens[b] .. lens[b] + counts[b] - 1.
+ *
+ * The call serves a whole prompt or a compressed cache (cache_len = 0,
+ * n_new = its length), a chunk of a prefill and a single token alike.
+ * counts = NULL: every sequence gets n_new rows; otherwise counts[b] (int32,
+ * on the device) of them, the rows behind being padding that is not read.
+ * counts[b] is clamped to [0, n_new] and to the room that is left.
+ * In:  K_new, V_new [B, H_kv, n_new, d] (kv_dtype; must not overlap the
+ *      cache); 0 <= cache_len, cache_len + n_new <= capacity where counts and
+ *      lens are NULL (otherwise cache_len <= capacity).
+ * In/out: the cache.  Entries in front of lens[b] and buffers behind the new
+ *      entries keep their contents.
+ * Workspace: none. */
+SELKV_API selkv_status selkv_cache8_write(const selkv_params* p, const selkv_cache8* c, const void* K_new,
+                                          const void* V_new, int32_t n_new, int32_t cache_len, const int32_t* lens,
+                                          const int32_t* counts, hipStream_t stream);
+
+/* Read entries first .. first + count - 1 of every sequence back as rows in
+ * the storage type: code * scale rounded once to kv_dtype, the rows of the
+ * open block as they are (what the decode attends over).
+ * In:  the cache; 0 <= first, count >= 1, first + count <= capacity.
+ * Out: K_out, V_out [B, H_kv, count, d] (kv_dtype); rows of entries that a
+ *      sequence does not hold are left as they were.
+ * Workspace: none. */
+SELKV_API selkv_status selkv_cache8_read(const selkv_params* p, const selkv_cache8* c, void* K_out, void* V_out,
+                                         int32_t first, int32_t count, int32_t cache_len, const int32_t* lens,
+                                         hipStream_t stream);
+
+/* Bytes of scratch that selkv_decode8_attn and selkv_decode8_append need for
+ * `p` and `c`, at every cache_len up to c->capacity (of `c` only the sizes
+ * are read).  Host-only. */
+SELKV_API selkv_status selkv_decode8_workspace_size(const selkv_params* p, const selkv_cache8* c, size_t* bytes);
+
+/* Decode over the 8-bit cache: selkv_decode_attn with the entries' values.
+ *
+ * out[b, h] = sum_e softmax_e(scale * q[b, h] . K[b, h/G, e] + bias[b, h/G, e]) V[b, h/G, e]
+ * over the entries e < lens[b].  bias may be NULL (bitwise the result of a
+ * zero bias); a bias of -inf masks its entry whatever the entry holds.  A
+ * sequence with no entries, or none that is not masked, gives out = 0.
+ * Queries are not quantised and all sums are fp32.
+ * In:  q [B, H_kv*G, d] (kv_dtype); bias [B, H_kv, capacity] fp32 or NULL;
+ *      0 <= cache_len <= capacity.  Uses params batch, n_heads_kv, group
+ *      (1..8), head_dim, kv_dtype and scale only.
+ * Out: out [B, H_kv*G, d] fp32.
+ * Workspace: selkv_decode8_workspace_size(); no initialisation is needed.
+ *      Calls that may overlap in time need separate workspaces. */
+SELKV_API selkv_status selkv_decode8_attn(const selkv_params* p, const selkv_cache8* c, const void* q,
+                                          const float* bias, int32_t cache_len, const int32_t* lens, float* out,
+                                          void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* One generation step over a growing 8-bit cache: the new token becomes entry
+ * lens[b] (bias 0, and 0 is stored in bias there when bias is given) and the
+ * step attends over lens[b] + 1 entries, the new one and the others of its
+ * block with the rows as given.  The new row is stored in the tail; when it
+ * completes the block the call quantises the block for the later steps.
+ * In:  q [B, H_kv*G, d]; k_new, v_new [B, H_kv, d] (kv_dtype; must not
+ *      overlap the cache); 0 <= cache_len < capacity.
+ * In/out: the cache; bias [B, H_kv, capacity] fp32 or NULL.
+ * Out: out [B, H_kv*G, d] fp32.
+ * Workspace: as selkv_decode8_attn. */
+SELKV_API selkv_status selkv_decode8_append(const selkv_params* p, const selkv_cache8* c, const void* q,
+                                            const void* k_new, const void* v_new, float* bias, int32_t cache_len,
+                                            const int32_t* lens, float* out, void* ws, size_t ws_bytes,
+                                            hipStream_t stream);
+
 /* Static, NUL-terminated description of a status code. */
 SELKV_API const char* selkv_status_string(selkv_status s);
 

@@ -1,0 +1,162 @@
+// Device code shared by the kernels of the 8-bit cache (cache8.hip,
+// decode8.hip): lengths, the quantisation of a block, code conversions.
+//
+// A block is T tokens of one KV head.  With a the largest magnitude of its
+// finite elements and top the largest code (127, or e4m3's 448):
+//   scale = a / top,  code = rne(clamp(x * (top / a))).
+// K codes are rows of d bytes; V codes are tiles of 16 tokens, channel by
+// channel (byte ((t / 16) * d + c) * 16 + t % 16), so that a lane that wants a
+// channel's values for a run of tokens, as P V on the matrix cores does,
+// reads them with one 16-byte load.
+#pragma once
+
+#include "common.hpp"
+#include "internal.hpp"
+
+namespace selkv {
+
+constexpr float kTinyBlock = 0x1p-100f;   // below it top / a nears the end of fp32: the block is stored as zeros
+
+template <int CODE>
+__device__ __forceinline__ constexpr float code_top() { return CODE == SELKV_I8 ? 127.f : 448.f; }
+
+// Entries of sequence b: lens[b] where lens is set, at most cache_len; negative: the sequence takes no part.
+__device__ __forceinline__ int entries_of(const Lens8& n, int b) {
+  return n.lens ? min(n.lens[b], n.cache_len) : n.cache_len;
+}
+
+// Four elements of a row in storage type T, raw.
+template <typename T> struct Quad;
+template <> struct Quad<float> {
+  uint4 w;
+  __device__ __forceinline__ void load(const char* p) { w = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void store(char* p) const { *reinterpret_cast<uint4*>(p) = w; }
+  __device__ __forceinline__ float get(int e) const {
+    return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w);
+  }
+  __device__ __forceinline__ void set(const float (&x)[4]) {
+    w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+template <> struct Quad<bf16_t> {
+  uint2 w;
+  __device__ __forceinline__ void load(const char* p) { w = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void store(char* p) const { *reinterpret_cast<uint2*>(p) = w; }
+  __device__ __forceinline__ float get(int e) const {
+    const uint32_t x = e < 2 ? w.x : w.y;
+    return __uint_as_float((e & 1) ? (x & 0xffff0000u) : (x << 16));
+  }
+  __device__ __forceinline__ void set(const float (&x)[4]) {
+    w.x = f32_to_bf16(x[0]) | ((uint32_t)f32_to_bf16(x[1]) << 16);
+    w.y = f32_to_bf16(x[2]) | ((uint32_t)f32_to_bf16(x[3]) << 16);
+  }
+};
+
+// |x|, or 0 for an infinity or a NaN.
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a < __builtin_huge_valf() ? a : 0.f;
+}
+
+// Codes of four values, in the bytes of one word.  fminf / fmaxf drop a NaN, so it is set to 0 first.
+template <int CODE>
+__device__ __forceinline__ uint32_t encode4(float x0, float x1, float x2, float x3, float inv) {
+  float y[4] = {x0 * inv, x1 * inv, x2 * inv, x3 * inv};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = y[i] == y[i] ? y[i] : 0.f;
+    y[i] = fminf(fmaxf(y[i], -code_top<CODE>()), code_top<CODE>());
+  }
+  if constexpr (CODE == SELKV_I8) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int)rintf(y[i]) & 0xffu) << (8 * i);
+    return w;
+  } else {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+    return (uint32_t)w;
+  }
+}
+
+// The value (without the scale) of byte B of a word of codes.
+template <int CODE, int B>
+__device__ __forceinline__ float decode1(uint32_t w) {
+  if constexpr (CODE == SELKV_I8) return (float)(int8_t)(w >> (8 * B));
+  else return __builtin_amdgcn_cvt_f32_fp8((int)w, B);
+}
+
+template <int CODE>
+__device__ __forceinline__ void decode4(uint32_t w, float (&x)[4]) {
+  x[0] = decode1<CODE, 0>(w);
+  x[1] = decode1<CODE, 1>(w);
+  x[2] = decode1<CODE, 2>(w);
+  x[3] = decode1<CODE, 3>(w);
+}
+
+// Quantises blocks of K or V by the first 256 threads of a workgroup.  A
+// thread holds 16 tokens x 4 channels of its block: d/4 threads side by side
+// read a row (256 or 512 bytes together), and each has whole 16-token runs of
+// its channels, so V's tiles need no exchange between threads.  Per block
+// block/16 * d/4 = 16 .. 256 threads.  Every thread of the workgroup calls it
+// (it has barriers); `on`: the thread has a block.
+// row(i): address of the thread's channels in token i of its tile; codes,
+// scale: of the thread's block (codes at its first entry).
+struct BlockThread {
+  int sub, tile, c4;   // block among those of the workgroup, 16-token tile in it, channel / 4
+};
+
+template <int D>
+__device__ __forceinline__ BlockThread block_thread(int tid, int block) {
+  const int per = block / 16 * (D / 4);
+  const int u = tid % per;
+  return BlockThread{tid / per, u / (D / 4), u % (D / 4)};
+}
+
+template <typename T, int D, int CODE, typename Row>
+__device__ __forceinline__ void quantise_blocks(bool on, const BlockThread& bt, int block, bool is_v, Row row,
+                                                char* codes, float* scale, float (&s_max)[4]) {
+  Quad<T> x[16];
+  float a = 0.f;
+  if (on) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i].load(row(i));
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a = fmaxf(a, finite_abs(x[i].get(e)));
+  }
+  const int per = block / 16 * (D / 4);   // a power of two, 16 .. 256
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1)
+    if (off < per) a = fmaxf(a, xor_shfl(a, off));
+  if (per > 64) {                          // uniform: the waves of a block meet in LDS
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0 && wave < 4) s_max[wave] = a;
+    __syncthreads();
+    const int w0 = (wave & 3) & ~(per / 64 - 1);
+    for (int w = 0; w < per / 64; ++w) a = fmaxf(a, s_max[w0 + w]);
+  }
+  if (!on) return;
+  const bool tiny = a < kTinyBlock;
+  const float inv = tiny ? 0.f : code_top<CODE>() / a;
+  if (bt.tile == 0 && bt.c4 == 0) *scale = tiny ? 0.f : a / code_top<CODE>();
+  if (!is_v) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      *reinterpret_cast<uint32_t*>(codes + (size_t)(bt.tile * 16 + i) * D + bt.c4 * 4) =
+          encode4<CODE>(x[i].get(0), x[i].get(1), x[i].get(2), x[i].get(3), inv);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      Chunk16 ch;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        ch.w[w] = encode4<CODE>(x[4 * w].get(e), x[4 * w + 1].get(e), x[4 * w + 2].get(e), x[4 * w + 3].get(e), inv);
+      store16(codes + ((size_t)bt.tile * D + bt.c4 * 4 + e) * 16, ch);
+    }
+  }
+}
+
+}  // namespace selkv

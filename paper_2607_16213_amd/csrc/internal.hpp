@@ -120,4 +120,40 @@ hipError_t launch_decode(int64_t heads, int n_heads_kv, int cache_len, int strid
                          const float* bias, float* out, void* ws, hipStream_t st, const void* k_new = nullptr,
                          const void* v_new = nullptr);
 
+// An 8-bit cache as the kernels see it.
+struct Cache8 {
+  int code;            // selkv_code8
+  int block, capacity; // tokens per scale, entries per KV head
+  char* K;
+  char* V;
+  float* k_scale;
+  float* v_scale;
+  char* k_tail;
+  char* v_tail;
+};
+
+// Lengths of the sequences: cache_len each, or lens[b] where lens is set.
+struct Lens8 {
+  int cache_len;
+  const int32_t* lens;
+};
+
+struct Decode8Plan {
+  int nsplit;          // workgroups per KV head over the codes (1: one workgroup takes the head, tail included)
+  int slots;           // partials per KV head
+  size_t ml_bytes;     // (max, sum) partials, at the start of the workspace
+  size_t bytes;
+};
+
+Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G);
+
+hipError_t launch_cache8_write(int64_t heads, int hkv, int d, int dtype, const Cache8& c, const Lens8& n,
+                               const int32_t* counts, const void* K_new, const void* V_new, int n_new, hipStream_t st);
+hipError_t launch_cache8_read(int64_t heads, int hkv, int d, int dtype, const Cache8& c, const Lens8& n, void* K_out,
+                              void* V_out, int first, int count, hipStream_t st);
+// k_new / v_new set: the step appends (bias is written at the new entry, if there is one)
+hipError_t launch_decode8(int64_t heads, int hkv, int d, int G, int dtype, float scale, const Decode8Plan& plan,
+                          const Cache8& c, const Lens8& n, const void* q, float* bias, const void* k_new,
+                          const void* v_new, float* out, void* ws, hipStream_t st);
+
 }  // namespace selkv

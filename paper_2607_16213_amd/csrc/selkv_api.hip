@@ -138,6 +138,45 @@ selkv_status check_ws(void* ws, size_t ws_bytes, size_t need) {
   return SELKV_OK;
 }
 
+// Arguments that every call on an 8-bit cache shares: the fields of selkv_params that they use and the cache.
+// Sizes only where `buffers` is false.
+selkv_status check_cache8(const selkv_params* p, const selkv_cache8* c, bool buffers) {
+  if (!p || p->struct_size != sizeof(selkv_params)) return SELKV_EINVAL;
+  if (!c || c->struct_size != sizeof(selkv_cache8)) return SELKV_EINVAL;
+  if (p->kv_dtype != SELKV_F32 && p->kv_dtype != SELKV_BF16) return SELKV_EDTYPE;
+  if (c->code != SELKV_I8 && c->code != SELKV_E4M3) return SELKV_EDTYPE;
+  if (p->batch < 1 || p->n_heads_kv < 1) return SELKV_EINVAL;
+  if (p->head_dim != 64 && p->head_dim != 128) return SELKV_EUNSUPPORTED;
+  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) return SELKV_EUNSUPPORTED;
+  if (c->capacity < c->block || c->capacity % c->block != 0) return SELKV_EINVAL;
+  if (c->capacity > (1 << 28)) return SELKV_EUNSUPPORTED;
+  if ((int64_t)p->batch * p->n_heads_kv > 65535) return SELKV_EUNSUPPORTED;   // grid y dimension
+  if (!buffers) return SELKV_OK;
+  if (!c->K || !c->V || !c->k_scale || !c->v_scale || !c->k_tail || !c->v_tail) return SELKV_EINVAL;
+  if (!aligned(c->K, 16) || !aligned(c->V, 16) || !aligned(c->k_tail, 16) || !aligned(c->v_tail, 16) ||
+      !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4))
+    return SELKV_EALIGN;
+  return SELKV_OK;
+}
+
+// ... and those of the two decode calls on one.
+selkv_status check_decode8(const selkv_params* p, const selkv_cache8* c, const void* q, const float* bias,
+                           int32_t cache_len, const int32_t* lens, float* out) {
+  const selkv_status st = check_cache8(p, c, true);
+  if (st != SELKV_OK) return st;
+  if (p->group < 1 || cache_len < 0 || cache_len > c->capacity) return SELKV_EINVAL;
+  if (p->group > 8) return SELKV_EUNSUPPORTED;
+  if (!(p->scale >= 0.f) || !isfinite(p->scale)) return SELKV_EINVAL;
+  if (!q || !out) return SELKV_EINVAL;
+  if (!aligned(q, 16) || !aligned(bias, 4) || !aligned(lens, 4) || !aligned(out, 16)) return SELKV_EALIGN;
+  return SELKV_OK;
+}
+
+Cache8 view_cache8(const selkv_cache8* c) {
+  return Cache8{c->code, c->block, c->capacity, static_cast<char*>(c->K), static_cast<char*>(c->V), c->k_scale,
+                c->v_scale, static_cast<char*>(c->k_tail), static_cast<char*>(c->v_tail)};
+}
+
 selkv_status check_merge_args(const Shape& s, const void* K, const void* V, const float* attn, const float* vnorm,
                               const int32_t* kept_idx, const int32_t* evicted_idx, void* K_out, void* V_out,
                               int32_t* target, float* gate) {
@@ -443,6 +482,79 @@ SELKV_API selkv_status selkv_decode_append(const selkv_params* p, const void* q,
   // one launch: the new entry is read from k_new / v_new and stored into the cache on the way
   return hip_status(launch_decode(heads, p->n_heads_kv, cache_len + 1, capacity, p->head_dim, p->group,
                                   p->kv_dtype, eff_scale(p), plan, q, K, V, bias, out, ws, stream, k_new, v_new));
+}
+
+SELKV_API void selkv_cache8_init(selkv_cache8* c) {
+  if (!c) return;
+  memset(c, 0, sizeof(*c));
+  c->struct_size = sizeof(selkv_cache8);
+  c->code = SELKV_I8;
+  c->block = 64;
+}
+
+SELKV_API selkv_status selkv_cache8_write(const selkv_params* p, const selkv_cache8* c, const void* K_new,
+                                          const void* V_new, int32_t n_new, int32_t cache_len, const int32_t* lens,
+                                          const int32_t* counts, hipStream_t stream) {
+  const selkv_status st = check_cache8(p, c, true);
+  if (st != SELKV_OK) return st;
+  if (n_new < 1 || cache_len < 0 || cache_len > c->capacity || n_new > c->capacity) return SELKV_EINVAL;
+  if (!lens && !counts && n_new > c->capacity - cache_len) return SELKV_EINVAL;   // no room for the new entries
+  if (!K_new || !V_new) return SELKV_EINVAL;
+  if (!aligned(K_new, 16) || !aligned(V_new, 16) || !aligned(lens, 4) || !aligned(counts, 4)) return SELKV_EALIGN;
+  return hip_status(launch_cache8_write((int64_t)p->batch * p->n_heads_kv, p->n_heads_kv, p->head_dim, p->kv_dtype,
+                                        view_cache8(c), Lens8{cache_len, lens}, counts, K_new, V_new, n_new, stream));
+}
+
+SELKV_API selkv_status selkv_cache8_read(const selkv_params* p, const selkv_cache8* c, void* K_out, void* V_out,
+                                         int32_t first, int32_t count, int32_t cache_len, const int32_t* lens,
+                                         hipStream_t stream) {
+  const selkv_status st = check_cache8(p, c, true);
+  if (st != SELKV_OK) return st;
+  if (cache_len < 0 || cache_len > c->capacity) return SELKV_EINVAL;
+  if (first < 0 || count < 1 || first > c->capacity - count) return SELKV_EINVAL;
+  if (!K_out || !V_out) return SELKV_EINVAL;
+  if (!aligned(K_out, 16) || !aligned(V_out, 16) || !aligned(lens, 4)) return SELKV_EALIGN;
+  return hip_status(launch_cache8_read((int64_t)p->batch * p->n_heads_kv, p->n_heads_kv, p->head_dim, p->kv_dtype,
+                                       view_cache8(c), Lens8{cache_len, lens}, K_out, V_out, first, count, stream));
+}
+
+SELKV_API selkv_status selkv_decode8_workspace_size(const selkv_params* p, const selkv_cache8* c, size_t* bytes) {
+  if (!bytes) return SELKV_EINVAL;
+  const selkv_status st = check_cache8(p, c, false);
+  if (st != SELKV_OK) return st;
+  if (p->group < 1) return SELKV_EINVAL;
+  if (p->group > 8) return SELKV_EUNSUPPORTED;
+  *bytes = plan_decode8((int64_t)p->batch * p->n_heads_kv, c->capacity, p->head_dim, p->group).bytes;
+  return SELKV_OK;
+}
+
+SELKV_API selkv_status selkv_decode8_attn(const selkv_params* p, const selkv_cache8* c, const void* q,
+                                          const float* bias, int32_t cache_len, const int32_t* lens, float* out,
+                                          void* ws, size_t ws_bytes, hipStream_t stream) {
+  selkv_status st = check_decode8(p, c, q, bias, cache_len, lens, out);
+  if (st != SELKV_OK) return st;
+  const int64_t heads = (int64_t)p->batch * p->n_heads_kv;
+  const Decode8Plan plan = plan_decode8(heads, cache_len, p->head_dim, p->group);
+  if ((st = check_ws(ws, ws_bytes, plan.bytes)) != SELKV_OK) return st;
+  return hip_status(launch_decode8(heads, p->n_heads_kv, p->head_dim, p->group, p->kv_dtype, eff_scale(p), plan,
+                                   view_cache8(c), Lens8{cache_len, lens}, q, const_cast<float*>(bias), nullptr,
+                                   nullptr, out, ws, stream));
+}
+
+SELKV_API selkv_status selkv_decode8_append(const selkv_params* p, const selkv_cache8* c, const void* q,
+                                            const void* k_new, const void* v_new, float* bias, int32_t cache_len,
+                                            const int32_t* lens, float* out, void* ws, size_t ws_bytes,
+                                            hipStream_t stream) {
+  selkv_status st = check_decode8(p, c, q, bias, cache_len, lens, out);
+  if (st != SELKV_OK) return st;
+  if (cache_len >= c->capacity) return SELKV_EINVAL;                 // no room for the new entry
+  if (!k_new || !v_new) return SELKV_EINVAL;
+  if (!aligned(k_new, 16) || !aligned(v_new, 16)) return SELKV_EALIGN;
+  const int64_t heads = (int64_t)p->batch * p->n_heads_kv;
+  const Decode8Plan plan = plan_decode8(heads, cache_len, p->head_dim, p->group);
+  if ((st = check_ws(ws, ws_bytes, plan.bytes)) != SELKV_OK) return st;
+  return hip_status(launch_decode8(heads, p->n_heads_kv, p->head_dim, p->group, p->kv_dtype, eff_scale(p), plan,
+                                   view_cache8(c), Lens8{cache_len, lens}, q, bias, k_new, v_new, out, ws, stream));
 }
 
 SELKV_API const char* selkv_status_string(selkv_status s) {

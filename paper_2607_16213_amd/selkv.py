@@ -28,6 +28,8 @@ GATE_MODES = {"cosine": GATE_COSINE, "drop": GATE_DROP, "merge_all": GATE_MERGE_
 ROUTE_MODES = {"bucket": ROUTE_BUCKET, "full_cosine": ROUTE_FULL_COSINE, "bucket_nearest": ROUTE_BUCKET_NEAREST,
                "coattn": ROUTE_COATTN}
 SELECT_MODES = {"per_head": SELECT_PER_HEAD, "union": SELECT_UNION}
+CODE_I8, CODE_E4M3 = 0, 1
+CODES8 = {"int8": CODE_I8, "e4m3": CODE_E4M3}
 
 
 class SelkvError(RuntimeError):
@@ -61,12 +63,29 @@ class Params(ctypes.Structure):
     ]
 
 
+class Cache8Struct(ctypes.Structure):
+    """selkv_cache8."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("code", ctypes.c_int32),
+        ("block", ctypes.c_int32),
+        ("capacity", ctypes.c_int32),
+        ("K", ctypes.c_void_p),
+        ("V", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("k_tail", ctypes.c_void_p),
+        ("v_tail", ctypes.c_void_p),
+    ]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run paper_2607_16213_amd.build.build() first")
     lib = ctypes.CDLL(LIB_PATH)
     vp, sz, i32, fp, ip = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p
     P = ctypes.POINTER(Params)
+    C8 = ctypes.POINTER(Cache8Struct)
     sigs = {
         "selkv_params_init": (None, [P]),
         "selkv_budget": (ctypes.c_int, [P, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32)]),
@@ -81,6 +100,12 @@ def _load():
         "selkv_decode_attn_noalloc": (ctypes.c_int, [P, vp, vp, vp, fp, i32, fp, vp]),
         "selkv_rope_reposition": (ctypes.c_int, [P, ip, vp, ctypes.c_double, vp]),
         "selkv_decode_append": (ctypes.c_int, [P, vp, vp, vp, vp, vp, fp, i32, i32, fp, vp, sz, vp]),
+        "selkv_cache8_init": (None, [C8]),
+        "selkv_cache8_write": (ctypes.c_int, [P, C8, vp, vp, i32, i32, ip, ip, vp]),
+        "selkv_cache8_read": (ctypes.c_int, [P, C8, vp, vp, i32, i32, i32, ip, vp]),
+        "selkv_decode8_workspace_size": (ctypes.c_int, [P, C8, ctypes.POINTER(sz)]),
+        "selkv_decode8_attn": (ctypes.c_int, [P, C8, vp, fp, i32, ip, fp, vp, sz, vp]),
+        "selkv_decode8_append": (ctypes.c_int, [P, C8, vp, vp, vp, fp, i32, ip, fp, vp, sz, vp]),
         "selkv_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "selkv_abi_version": (ctypes.c_int32, []),
     }
@@ -367,6 +392,151 @@ def decode_append(p, q, k_new, v_new, K, V, bias_io, cache_len, out, ws, stream=
         raise SelkvError(st, "selkv_decode_append")
 
 
+class Cache8:
+    """A KV cache held in 8 bits: its buffers and the selkv_cache8 that names them.
+
+    `capacity` entries per KV head (rounded up to whole blocks) as `code`
+    ("int8" or "e4m3") with one scale per `block` tokens; the rows of the last,
+    incomplete block stay in the storage type.  `over` takes existing buffers.
+    The lengths are the caller's: every call is given them."""
+
+    def __init__(self, p: Params, capacity: int, device, code: str = "int8", block: int = 64):
+        if block not in (16, 32, 64, 128):
+            raise ValueError("block must be 16, 32, 64 or 128")
+        B, H, d, dt = p.batch, p.n_heads_kv, p.head_dim, _kvdt(p)
+        cap = -(-capacity // block) * block
+        ct = torch.int8 if CODES8[code] == CODE_I8 else torch.float8_e4m3fn
+        zeros = lambda shape, t: torch.zeros(shape, dtype=t, device=device)
+        self._take(p, torch.zeros((B, H, cap, d), dtype=torch.int8, device=device).view(ct),
+                   torch.zeros((B, H, cap // 16, d, 16), dtype=torch.int8, device=device).view(ct),
+                   zeros((B, H, cap // block), _F32), zeros((B, H, cap // block), _F32), zeros((B, H, block, d), dt),
+                   zeros((B, H, block, d), dt))
+
+    @classmethod
+    def over(cls, p: Params, K, V, k_scale, v_scale, k_tail, v_tail) -> "Cache8":
+        """A cache in buffers that the caller owns (the layouts of include/selkv.h): the type of the codes is that of
+        K, the block the rows of k_tail, the capacity K.shape[2]."""
+        c = cls.__new__(cls)
+        c._take(p, K, V, k_scale, v_scale, k_tail, v_tail)
+        return c
+
+    def _take(self, p, K, V, k_scale, v_scale, k_tail, v_tail):
+        B, H, d, dt = p.batch, p.n_heads_kv, p.head_dim, _kvdt(p)
+        if K.dtype not in (torch.int8, torch.float8_e4m3fn):
+            raise ValueError(f"K has dtype {K.dtype}, expected torch.int8 or torch.float8_e4m3fn")
+        if K.dim() != 4 or k_tail.dim() != 4:
+            raise ValueError("K and k_tail must have four dimensions")
+        cap, block = K.shape[2], k_tail.shape[2]
+        if block not in (16, 32, 64, 128) or cap < block or cap % block:
+            raise ValueError(f"a cache of {cap} entries and a tail of {block} rows: the tail must have 16, 32, 64 or 128 "
+                             "rows and the capacity be whole blocks of them")
+        _dev(K, (B, H, cap, d), K.dtype, "K"); _dev(V, (B, H, cap // 16, d, 16), K.dtype, "V")
+        _dev(k_scale, (B, H, cap // block), _F32, "k_scale"); _dev(v_scale, (B, H, cap // block), _F32, "v_scale")
+        _dev(k_tail, (B, H, block, d), dt, "k_tail"); _dev(v_tail, (B, H, block, d), dt, "v_tail")
+        self.K, self.V, self.k_scale, self.v_scale, self.k_tail, self.v_tail = K, V, k_scale, v_scale, k_tail, v_tail
+        self.device = K.device
+        if any(t.device != K.device for t in (V, k_scale, v_scale, k_tail, v_tail)):
+            raise ValueError("the buffers of a cache must be on one device")
+        self.capacity, self.block = cap, block
+        self._of = (B, H, d, p.kv_dtype)
+        self.c = Cache8Struct()
+        lib.selkv_cache8_init(self.c)
+        self.c.code = CODE_I8 if K.dtype == torch.int8 else CODE_E4M3
+        self.c.block, self.c.capacity = block, cap
+        self.c.K, self.c.V, self.c.k_scale, self.c.v_scale = (t.data_ptr() for t in (K, V, k_scale, v_scale))
+        self.c.k_tail, self.c.v_tail = k_tail.data_ptr(), v_tail.data_ptr()
+
+
+def _check_cache8(p, cache, tensors, lens, counts, stream):
+    """Checks the cache against p and the current device, and (tensor, shape, dtype, name) of every tensor.  The launch
+    goes to the current device, so all of them have to be there."""
+    if cache._of != (p.batch, p.n_heads_kv, p.head_dim, p.kv_dtype):
+        raise ValueError(f"the cache was made for (batch, n_heads_kv, head_dim, kv_dtype) = {cache._of}")
+    dev = cache.device
+    if dev.index != torch.cuda.current_device() or (stream is not None and stream.device != dev):
+        raise ValueError(f"the cache is on {dev}: it must be the current device, and that of the stream")
+    if lens is not None:
+        tensors += ((lens, (p.batch,), _I32, "lens"),)
+    if counts is not None:
+        tensors += ((counts, (p.batch,), _I32, "counts"),)
+    for t, shape, dtype, name in tensors:
+        if not _ok(t, shape, dtype) or t.device != dev:
+            _dev(t, shape, dtype, name)
+            raise ValueError(f"{name} is on {t.device}, the cache on {dev}")
+
+
+def cache8_write(p, cache, K_new, V_new, cache_len, lens=None, counts=None, stream=None):
+    """Append rows K_new, V_new [B, H, n_new, d] behind the cache_len (or lens[b]) entries of every sequence;
+    counts [B] says how many of them each sequence gets (all n_new without it)."""
+    if K_new.dim() != 4:
+        raise ValueError("K_new must have four dimensions")
+    n_new = K_new.shape[2]
+    new, dt = (p.batch, p.n_heads_kv, n_new, p.head_dim), _kvdt(p)
+    _check_cache8(p, cache, ((K_new, new, dt, "K_new"), (V_new, new, dt, "V_new")), lens, counts, stream)
+    if n_new == 0:
+        return
+    st = lib.selkv_cache8_write(p, cache.c, K_new.data_ptr(), V_new.data_ptr(), n_new, int(cache_len), _ptr(lens),
+                                _ptr(counts), _stream(stream))
+    if st:
+        raise SelkvError(st, "selkv_cache8_write")
+
+
+def cache8_read(p, cache, K_out, V_out, cache_len, first=0, lens=None, stream=None):
+    """Entries first .. first + K_out.shape[2] - 1 as rows in the storage type; rows of entries that a sequence does
+    not hold are left as they were."""
+    if K_out.dim() != 4:
+        raise ValueError("K_out must have four dimensions")
+    count = K_out.shape[2]
+    out, dt = (p.batch, p.n_heads_kv, count, p.head_dim), _kvdt(p)
+    _check_cache8(p, cache, ((K_out, out, dt, "K_out"), (V_out, out, dt, "V_out")), lens, None, stream)
+    if count == 0:
+        return
+    st = lib.selkv_cache8_read(p, cache.c, K_out.data_ptr(), V_out.data_ptr(), int(first), count, int(cache_len),
+                               _ptr(lens), _stream(stream))
+    if st:
+        raise SelkvError(st, "selkv_cache8_read")
+
+
+def decode8_workspace_bytes(p: Params, cache: Cache8) -> int:
+    b = ctypes.c_size_t()
+    _check(lib.selkv_decode8_workspace_size(p, cache.c, ctypes.byref(b)), "selkv_decode8_workspace_size")
+    return b.value
+
+
+def decode8_workspace(p: Params, cache: Cache8) -> torch.Tensor:
+    """Scratch for decode8_attn and decode8_append at every length up to the capacity (needs no initialisation)."""
+    return torch.zeros(max(decode8_workspace_bytes(p, cache), 1), dtype=torch.uint8, device=cache.device)
+
+
+def decode8_attn(p, cache, q, bias_in, cache_len, out, ws, lens=None, stream=None):
+    """Biased decode over the 8-bit cache; bias_in [B, H, capacity] or None."""
+    B, H = p.batch, p.n_heads_kv
+    qs = (B, H * p.group, p.head_dim)
+    ts = ((q, qs, _kvdt(p), "q"), (out, qs, _F32, "out"))
+    if bias_in is not None:
+        ts += ((bias_in, (B, H, cache.capacity), _F32, "bias"),)
+    _check_cache8(p, cache, ts, lens, None, stream)
+    st = lib.selkv_decode8_attn(p, cache.c, q.data_ptr(), _ptr(bias_in), int(cache_len), _ptr(lens), out.data_ptr(),
+                                _ptr(ws), _nbytes(ws), _stream(stream))
+    if st:
+        raise SelkvError(st, "selkv_decode8_attn")
+
+
+def decode8_append(p, cache, q, k_new, v_new, bias_io, cache_len, out, ws, lens=None, stream=None):
+    """Append (k_new, v_new) [B, H, d] at entry cache_len (or lens[b]; bias 0 there) and attend over the entries with
+    it.  lens is read only: advance it after the call."""
+    B, H, d = p.batch, p.n_heads_kv, p.head_dim
+    dt, qs = _kvdt(p), (B, H * p.group, d)
+    ts = ((q, qs, dt, "q"), (k_new, (B, H, d), dt, "k_new"), (v_new, (B, H, d), dt, "v_new"), (out, qs, _F32, "out"))
+    if bias_io is not None:
+        ts += ((bias_io, (B, H, cache.capacity), _F32, "bias"),)
+    _check_cache8(p, cache, ts, lens, None, stream)
+    st = lib.selkv_decode8_append(p, cache.c, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _ptr(bias_io),
+                                  int(cache_len), _ptr(lens), out.data_ptr(), _ptr(ws), _nbytes(ws), _stream(stream))
+    if st:
+        raise SelkvError(st, "selkv_decode8_append")
+
+
 class Compressor:
     """Owns the output and scratch tensors of one problem size and runs the
     compression calls (score, select, [route_coattn,] merge_bias, or merge then
@@ -410,6 +580,17 @@ class Compressor:
             bias(p, self.attn, self.kept, self.evicted, self.target, self.gate, self.bias, self.ws_merge, stream)
         return self
 
+    def store8(self, cache: Cache8, bias_out=None, stream=None):
+        """Write the compressed cache of the last run into an 8-bit cache from its start (it then holds m entries);
+        bias_out [B, H, capacity], if given, gets the biases of those entries."""
+        p = self.p
+        cache8_write(p, cache, self.K_out, self.V_out, 0, stream=stream)
+        if bias_out is not None:
+            _dev(bias_out, (p.batch, p.n_heads_kv, cache.capacity), _F32, "bias")
+            with torch.cuda.stream(stream):   # the current stream where none is given
+                bias_out[:, :, :self.m].copy_(self.bias)
+        return cache
+
     def outputs(self):
         return dict(score=self.score, attn=self.attn, vnorm=self.vnorm, kept=self.kept, evicted=self.evicted,
                     K_out=self.K_out, V_out=self.V_out, target=self.target, gate=self.gate, bias=self.bias)
@@ -427,4 +608,26 @@ class Decoder:
     def run(self, q, K, V, bias_in=None, out=None, stream=None):
         o = self.out if out is None else out
         decode_attn(self.p, q, K, V, bias_in, o, self.ws, stream)
+        return o
+
+
+class Decoder8:
+    """Owns the split-K workspace and the output of decode over one 8-bit cache."""
+
+    def __init__(self, p: Params, cache: Cache8):
+        self.p, self.cache = p, cache
+        self.ws = decode8_workspace(p, cache)
+        self.out = torch.empty((p.batch, p.n_heads_kv * p.group, p.head_dim), dtype=torch.float32,
+                               device=cache.device)
+
+    def run(self, q, cache_len, bias_in=None, lens=None, out=None, stream=None):
+        """Attend over the entries that are there."""
+        o = self.out if out is None else out
+        decode8_attn(self.p, self.cache, q, bias_in, cache_len, o, self.ws, lens, stream)
+        return o
+
+    def step(self, q, k_new, v_new, cache_len, bias_io=None, lens=None, out=None, stream=None):
+        """Append the new token and attend over the entries with it."""
+        o = self.out if out is None else out
+        decode8_append(self.p, self.cache, q, k_new, v_new, bias_io, cache_len, o, self.ws, lens, stream)
         return o
