@@ -11,8 +11,22 @@
 // one more workgroup per head the tail; each writes (max, sum, o[d]) per query
 // head to the workspace and a second kernel combines them in slot order.
 // Where one workgroup takes the whole head it writes the outputs itself.
-// Inside a wave a lane group of 16 lanes takes one entry, each lane d/16
-// channels; the running maximum and sum of the softmax are fp32.
+//
+// The codes go to the matrix cores as bf16, which holds every int8 and e4m3
+// number exactly.  A wave takes 64 entries at a time: four 16x16x32 tiles
+// S = K Q^T, then O^T += V^T P^T.  Of a tile's 16 columns the G <= 8 query
+// heads need at most 8, so column h + 8 carries what column h's bf16 leaves of
+// the same head, of an fp32 query and of a softmax weight: the next 8 bits, and
+// a second product the last 8, so both enter as the fp32 numbers they are (with
+// two terms the weight that dominates a peaked softmax was off by up to 2^-18,
+// 5.5e-6 of an output).  Which entry is which row of an S tile
+// is chosen so that a lane's logits are 16 consecutive entries, those whose V
+// codes it reads with one 16-byte load: P needs no exchange between lanes and
+// one scale of K and of V serves a lane's 64-entry step.  Scales stay out of the
+// products: K's multiplies the logits, V's the weights.
+// The running maximum and sum of the softmax, and all accumulators, are fp32.
+// The tail (and the appended token) are few rows, taken in fp32 by lane groups
+// of 16 lanes, each lane d/16 channels.
 // A masked entry (bias -inf) is left out by selection, so it may hold anything.
 #include "cache8.hpp"
 
@@ -92,12 +106,185 @@ __device__ __forceinline__ float weight_of(float m, float M) {
   return m == kNegInf ? 0.f : fast_exp2((m - M) * kLog2e);
 }
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));   // biases: aligned to an element only
+
+// Four codes as bf16 numbers (exact).
+template <int CODE>
+__device__ __forceinline__ uint2 codes_to_bf16(uint32_t w) {
+  if constexpr (CODE == SELKV_I8) {
+    float f[4];
+    decode4<CODE>(w, f);
+    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
+                      __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u));
+  } else {
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)));
+  }
+}
+
+// Half H (8 codes) of a 16-byte chunk as an MFMA operand.
+template <int CODE, int H>
+__device__ __forceinline__ bf16x8 half_to_bf16(const Chunk16& c) {
+  const uint2 a = codes_to_bf16<CODE>(c.w[2 * H]), b = codes_to_bf16<CODE>(c.w[2 * H + 1]);
+  const Chunk16 r = {a.x, a.y, b.x, b.y};
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+__device__ __forceinline__ float max_xor16(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_xor32(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Queries of a head as the MFMA B operand: lane (column, grp) holds channels
+// (4 j + grp) * 16 + 8 m .. + 7 of query column & 7, as K's codes come.
+template <typename T, int D>
+struct Query8 {
+  static constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
+  bf16x8 b[kParts][D / 64][2];
+  __device__ __forceinline__ void load(const char* q, int G, int col, int grp) {
+    const int h = col & 7;
+    const bool low = col >= 8;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const char* at = q + ((size_t)(h < G ? h : 0) * D + (4 * j + grp) * 16 + 8 * m) * sizeof(T);
+        if constexpr (sizeof(T) == 2) {
+          b[0][j][m] = __builtin_bit_cast(bf16x8, h < G ? load16(at) : zero16());
+        } else {
+          const Chunk16 c0 = load16(at), c1 = load16(at + 16);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float x = h < G ? __uint_as_float(i < 4 ? c0.w[i & 3] : c1.w[i & 3]) : 0.f;
+            const __bf16 hi = (__bf16)x;
+            const float r1 = x - (float)hi;
+            const __bf16 mid = (__bf16)r1;
+            const float r2 = r1 - (float)mid;
+            b[0][j][m][i] = low ? mid : hi;
+            b[1][j][m][i] = low ? (__bf16)0.f : (__bf16)r2;
+          }
+        }
+      }
+  }
+};
+
+// What a wave reads for 64 entries.
+template <int D>
+struct Codes8 {
+  Chunk16 k[4][D / 64];
+  Chunk16 v[D / 16];
+  f32x4u bias[4];
+  float ks, vs;
+};
+
+template <int D>
+__device__ __forceinline__ void load_codes(Codes8<D>& x, const char* Kh, const char* Vh, const float* ks,
+                                           const float* vs, const float* bh, int block_shift, int base, int e1,
+                                           int col, int grp) {
+  // 16-entry runs past the end are read at the group's first run instead and masked
+  const int krun = base + 16 * (col >> 2) < e1 ? 16 * (col >> 2) : 0;
+  const int vrun = base + 16 * grp < e1 ? 16 * grp : 0;
+  const char* kp = Kh + (size_t)(base + krun + (col & 3)) * D + grp * 16;
+  const char* vp = Vh + (size_t)(base + vrun) * D + col * 16;
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) x.k[s][j] = load16(kp + (4 * s) * D + j * 64);
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) x.v[c] = load16(vp + c * 256);
+  x.ks = ks[(base + vrun) >> block_shift];
+  x.vs = vs[(base + vrun) >> block_shift];
+  if (bh) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) x.bias[s] = *reinterpret_cast<const f32x4u*>(bh + base + vrun + 4 * s);
+  }
+}
+
+// Softmax state of a wave: lane (column, grp) keeps its column's maximum, the sum over its own entries and rows
+// 4 grp .. + 3 of every 16-channel tile of O^T.
+template <int D>
+struct Wave8 {
+  float m, l;
+  f32x4 o[D / 16];
+};
+
+template <typename T, int D, int CODE>
+__device__ __forceinline__ void attend_codes(Wave8<D>& st, const Codes8<D>& x, const Query8<T, D>& q, float scale,
+                                             bool has_bias, bool in, bool low) {
+  f32x4 s[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      const bf16x8 k0 = half_to_bf16<CODE, 0>(x.k[t][j]), k1 = half_to_bf16<CODE, 1>(x.k[t][j]);
+#pragma unroll
+      for (int p = 0; p < Query8<T, D>::kParts; ++p) {
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q.b[p][j][0], s[t], 0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q.b[p][j][1], s[t], 0, 0, 0);
+      }
+    }
+  }
+  const float c = scale * x.ks;
+  float mx = kNegInf;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float dot = s[t][r];
+      if constexpr (sizeof(T) == 4) dot += row_ror<8>(dot);   // both parts of the head's query
+      const float y = fmaf(dot, c, has_bias ? x.bias[t][r] : 0.f);
+      s[t][r] = in ? y : kNegInf;
+      mx = fmaxf(mx, s[t][r]);
+    }
+  mx = max_xor32(max_xor16(mx));
+  const float mnew = fmaxf(st.m, mx);
+  const float ref = mnew == kNegInf ? 0.f : mnew;   // nothing unmasked yet: every weight is 0
+  if (__any(mnew != st.m)) {
+    const float corr = fast_exp2((st.m - ref) * kLog2e);
+    st.l *= corr;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) st.o[i] *= corr;
+    st.m = mnew;
+  }
+  bf16x8 w[2], w_lo[2];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float p = fast_exp2((s[t][r] - ref) * kLog2e);
+      st.l += p;
+      const float y = p * x.vs;
+      const __bf16 hi = (__bf16)y;
+      const float r1 = y - (float)hi;
+      const __bf16 mid = (__bf16)r1;
+      w[t >> 1][(t & 1) * 4 + r] = low ? mid : hi;
+      w_lo[t >> 1][(t & 1) * 4 + r] = low ? (__bf16)0.f : (__bf16)(r1 - (float)mid);
+    }
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    const bf16x8 v0 = half_to_bf16<CODE, 0>(x.v[i]), v1 = half_to_bf16<CODE, 1>(x.v[i]);
+    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w_lo[0], st.o[i], 0, 0, 0);
+    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w_lo[1], st.o[i], 0, 0, 0);
+    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w[0], st.o[i], 0, 0, 0);
+    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w[1], st.o[i], 0, 0, 0);
+  }
+}
+
 template <typename T, int D, int CODE, bool APP>
-__global__ __launch_bounds__(kThreads) void decode8_kernel(DecodeArgs8 a) {
+__global__ __launch_bounds__(kThreads, 2) void decode8_kernel(DecodeArgs8 a) {
   constexpr int E = D / 16;
   constexpr int RB = D * (int)sizeof(T);
-  __shared__ float s_m[kWaves][kMaxG], s_l[kWaves][kMaxG];
-  __shared__ float s_o[kWaves][kMaxG][D];
+  // the waves' results over codes, then (where the workgroup takes both) those over the tail
+  __shared__ float s_m[2 * kWaves][kMaxG], s_l[2 * kWaves][kMaxG];
+  __shared__ __align__(16) float s_o[2 * kWaves][kMaxG][D];
   __shared__ float s_max[4];
   const int64_t head = blockIdx.y;
   const int slot = blockIdx.x, G = a.G;
@@ -109,46 +296,54 @@ __global__ __launch_bounds__(kThreads) void decode8_kernel(DecodeArgs8 a) {
   const int whole = active ? len / block * block : 0;    // entries held as codes
   const int rest = active ? len - whole : 0;             // rows in the tail
   const bool solo = a.slots == 1;
-  const bool tail_here = solo || slot == a.nsplit;
-
-  float q[kMaxG][E];
-#pragma unroll
-  for (int g = 0; g < kMaxG; ++g)
-    if (g < G) load_row<T, D>(a.q + ((size_t)head * G + g) * RB, col, q[g]);
-  State8<E> s;
-  s.clear();
-
+  const bool codes_here = slot < a.nsplit, tail_here = solo || slot == a.nsplit;
   const float* bh = a.bias ? a.bias + (size_t)head * cap : nullptr;
-  if (slot < a.nsplit) {
+  const char* qh = a.q + (size_t)head * G * RB;
+
+  if (codes_here) {
     const int groups = (whole + kGroup - 1) / kGroup;
     const int e0 = (int)((int64_t)groups * slot / a.nsplit) * kGroup;
     const int e1 = min((int)((int64_t)groups * (slot + 1) / a.nsplit) * kGroup, whole);
     const char* Kh = a.c.K + (size_t)head * cap * D;
     const char* Vh = a.c.V + (size_t)head * cap * D;
-    const float* ks = a.c.k_scale + (size_t)head * (cap / block);
-    const float* vs = a.c.v_scale + (size_t)head * (cap / block);
-    for (int e = e0 + wave * 4; e < e1; e += kWaves * 4) {   // e1 is a multiple of 16: the four entries are there
-      const int t = e + grp;
-      float k[E], v[E];
+    const int shift = 31 - __builtin_clz(block);
+    const float* ks = a.c.k_scale + (size_t)head * (cap >> shift);
+    const float* vs = a.c.v_scale + (size_t)head * (cap >> shift);
+    Query8<T, D> q;
+    q.load(qh, G, col, grp);
+    Wave8<D> st;
+    st.m = kNegInf;
+    st.l = 0.f;
 #pragma unroll
-      for (int i = 0; i < E; i += 4) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(Kh + (size_t)t * D + col * E + i);
-        float y[4];
-        decode4<CODE>(w, y);
-        k[i] = y[0]; k[i + 1] = y[1]; k[i + 2] = y[2]; k[i + 3] = y[3];
-      }
-      const float vsc = vs[t / block];
+    for (int i = 0; i < D / 16; ++i) st.o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int e = e0 + wave * kGroup; e < e1; e += kWaves * kGroup) {
+      Codes8<D> x;
+      load_codes<D>(x, Kh, Vh, ks, vs, bh, shift, e, e1, col, grp);
+      attend_codes<T, D, CODE>(st, x, q, a.scale, bh != nullptr, e + 16 * grp < e1, col >= 8);
+    }
+    st.l = add_xor32(add_xor16(st.l));
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        v[i] = decode1<CODE, 0>((uint8_t)Vh[((size_t)(t / 16) * D + col * E + i) * 16 + t % 16]) * vsc;
-      const float b = bh ? bh[t] : 0.f;
-      attend<E>(s, q, G, k, v, a.scale * ks[t / block], b, b != kNegInf);
+    for (int i = 0; i < D / 16; ++i) {
+      f32x4 o = st.o[i];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[r] += row_ror<8>(o[r]);   // both parts of the head's weights
+      if (col < G) *reinterpret_cast<f32x4*>(&s_o[wave][col][16 * i + 4 * grp]) = o;
+    }
+    if (col < G && grp == 0) {
+      s_m[wave][col] = st.m;
+      s_l[wave][col] = st.l;
     }
   }
-  if (tail_here && active) {
+  if (tail_here) {
+    float q[kMaxG][E];
+#pragma unroll
+    for (int g = 0; g < kMaxG; ++g)
+      if (g < G) load_row<T, D>(qh + (size_t)g * RB, col, q[g]);
+    State8<E> s;
+    s.clear();
     const char* kt = a.c.k_tail + (size_t)head * block * RB;
     const char* vt = a.c.v_tail + (size_t)head * block * RB;
-    const int rows = rest + (APP ? 1 : 0);
+    const int rows = active ? rest + (APP ? 1 : 0) : 0;
     for (int r0 = wave * 4; r0 < rows; r0 += kWaves * 4) {
       const int r = min(r0 + grp, rows - 1);
       const bool fresh = APP && r == rest;
@@ -158,39 +353,38 @@ __global__ __launch_bounds__(kThreads) void decode8_kernel(DecodeArgs8 a) {
       const float b = bh && !fresh ? bh[whole + r] : 0.f;
       attend<E>(s, q, G, k, v, a.scale, b, r0 + grp < rows && b != kNegInf);
     }
-  }
-
-  // the four lane groups of a wave, then the waves in order
+    // the four lane groups of a wave
+    const int at = codes_here ? kWaves + wave : wave;
 #pragma unroll
-  for (int g = 0; g < kMaxG; ++g) {
-    if (g >= G) break;
+    for (int g = 0; g < kMaxG; ++g) {
+      if (g >= G) break;
 #pragma unroll
-    for (int off = 16; off <= 32; off <<= 1) {
-      const float m2 = xor_shfl(s.m[g], off), l2 = xor_shfl(s.l[g], off);
-      const float M = fmaxf(s.m[g], m2);
-      const float c1 = weight_of(s.m[g], M), c2 = weight_of(m2, M);
-      s.l[g] = s.l[g] * c1 + l2 * c2;
+      for (int off = 16; off <= 32; off <<= 1) {
+        const float m2 = xor_shfl(s.m[g], off), l2 = xor_shfl(s.l[g], off);
+        const float M = fmaxf(s.m[g], m2);
+        const float c1 = weight_of(s.m[g], M), c2 = weight_of(m2, M);
+        s.l[g] = s.l[g] * c1 + l2 * c2;
 #pragma unroll
-      for (int e = 0; e < E; ++e) s.o[g][e] = s.o[g][e] * c1 + xor_shfl(s.o[g][e], off) * c2;
-      s.m[g] = M;
-    }
-    if (grp == 0) {
-      if (col == 0) {
-        s_m[wave][g] = s.m[g];
-        s_l[wave][g] = s.l[g];
+        for (int e = 0; e < E; ++e) s.o[g][e] = s.o[g][e] * c1 + xor_shfl(s.o[g][e], off) * c2;
+        s.m[g] = M;
       }
+      if (grp == 0) {
+        if (col == 0) {
+          s_m[at][g] = s.m[g];
+          s_l[at][g] = s.l[g];
+        }
 #pragma unroll
-      for (int e = 0; e < E; ++e) s_o[wave][g][col * E + e] = s.o[g][e];
+        for (int e = 0; e < E; ++e) s_o[at][g][col * E + e] = s.o[g][e];
+      }
     }
   }
   __syncthreads();
+  const int parts = solo ? 2 * kWaves : kWaves;
   for (int idx = threadIdx.x; idx < G * D; idx += kThreads) {
     const int g = idx / D, dd = idx % D;
     float M = kNegInf, l = 0.f, o = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][g]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < parts; ++w) M = fmaxf(M, s_m[w][g]);
+    for (int w = 0; w < parts; ++w) {
       const float c = weight_of(s_m[w][g], M);
       l = fmaf(s_l[w][g], c, l);
       o = fmaf(s_o[w][g][dd], c, o);
