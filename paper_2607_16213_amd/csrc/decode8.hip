@@ -8,9 +8,10 @@
 // block (the tail) and the token that the step appends.
 //
 // Split-K: a workgroup of four waves takes a run of entries of one KV head, and
-// one more workgroup per head the tail; each writes (max, sum, o[d]) per query
-// head to the workspace and a second kernel combines them in slot order.
-// Where one workgroup takes the whole head it writes the outputs itself.
+// one more workgroup per head the tail (slot 0, so that it starts first); each
+// writes (max, sum, o[d]) per query head to the workspace and a second kernel
+// combines them in slot order.  Where one workgroup takes the whole head, a
+// short cache or one of very many heads, it writes the outputs itself.
 //
 // The codes go to the matrix cores as bf16, which holds every int8 and e4m3
 // number exactly.  A wave takes 64 entries at a time: four 16x16x32 tiles
@@ -28,6 +29,8 @@
 // The tail (and the appended token) are few rows, taken in fp32 by lane groups
 // of 16 lanes, each lane d/16 channels.
 // A masked entry (bias -inf) is left out by selection, so it may hold anything.
+#include <algorithm>
+
 #include "cache8.hpp"
 
 namespace selkv {
@@ -36,9 +39,12 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kMaxG = 8;
-constexpr int kGroup = 64;            // entries that splits are whole multiples of
-constexpr int kTargetBlocks = 512;    // workgroups a launch aims at
-constexpr int kMaxSplit = 1024;
+constexpr int kTailG = 4;             // query heads of a pass over the tail: registers, shared with the codes' loop
+constexpr int kGroup = 64;            // entries of a wave's step; splits are whole multiples of them
+constexpr int kTargetBlocks = 768;    // workgroups that a launch aims at: three to a CU, what its registers hold
+constexpr int kMaxSplit = 512;
+constexpr int kSolo8Entries = 512;    // up to them a workgroup takes a head by itself
+constexpr int kFewSlots = 16;
 
 struct DecodeArgs8 {
   Cache8 c;
@@ -50,56 +56,9 @@ struct DecodeArgs8 {
   float2* part_ml;   // [heads, slots, G]
   const char* k_new; // APP
   const char* v_new;
-  int hkv, G, nsplit, slots;
+  int hkv, G, slots, chunk, block_shift;   // chunk: entries of a split
   float scale;
 };
-
-// Softmax state of one lane group: G heads, E channels of the lane.
-template <int E>
-struct State8 {
-  float m[kMaxG], l[kMaxG], o[kMaxG][E];
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int g = 0; g < kMaxG; ++g) {
-      m[g] = kNegInf;
-      l[g] = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[g][e] = 0.f;
-    }
-  }
-};
-
-// One entry per lane group: its logits, then the running softmax.  `in`: the entry counts (its k, v may be anything
-// where it does not).
-template <int E>
-__device__ __forceinline__ void attend(State8<E>& s, const float (&q)[kMaxG][E], int G, const float (&k)[E],
-                                       const float (&v)[E], float c, float bias, bool in) {
-#pragma unroll
-  for (int g = 0; g < kMaxG; ++g) {
-    if (g >= G) break;
-    float dot = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) dot = fmaf(q[g][e], k[e], dot);
-    dot = sum16(dot);
-    if (!in) continue;
-    const float x = fmaf(dot, c, bias);
-    const float mnew = fmaxf(s.m[g], x);
-    const float corr = fast_exp2((s.m[g] - mnew) * kLog2e);   // 0 while m is -inf
-    const float p = fast_exp2((x - mnew) * kLog2e);
-    s.l[g] = fmaf(s.l[g], corr, p);
-#pragma unroll
-    for (int e = 0; e < E; ++e) s.o[g][e] = fmaf(s.o[g][e], corr, p * v[e]);
-    s.m[g] = mnew;
-  }
-}
-
-template <typename T, int D>
-__device__ __forceinline__ void load_row(const char* row, int col, float (&x)[D / 16]) {
-  RawSlice<T, D> r;
-  r.load(row, col);
-#pragma unroll
-  for (int e = 0; e < D / 16; ++e) x[e] = r.get(e);
-}
 
 // Weight of partial (m, .) against the maximum M of all (0 where it is empty).
 __device__ __forceinline__ float weight_of(float m, float M) {
@@ -180,7 +139,7 @@ template <int D>
 struct Codes8 {
   Chunk16 k[4][D / 64];
   Chunk16 v[D / 16];
-  f32x4u bias[4];
+  f32x4u bias[2];   // of the entries whose weights the lane forms
   float ks, vs;
 };
 
@@ -203,17 +162,35 @@ __device__ __forceinline__ void load_codes(Codes8<D>& x, const char* Kh, const c
   x.vs = vs[(base + vrun) >> block_shift];
   if (bh) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) x.bias[s] = *reinterpret_cast<const f32x4u*>(bh + base + vrun + 4 * s);
+    for (int s = 0; s < 2; ++s)
+      x.bias[s] = *reinterpret_cast<const f32x4u*>(bh + base + vrun + (col & 8) + 4 * s);
   }
 }
 
-// Softmax state of a wave: lane (column, grp) keeps its column's maximum, the sum over its own entries and rows
-// 4 grp .. + 3 of every 16-channel tile of O^T.
+// Softmax state of a wave: lane (column, grp) keeps its column's maximum, the sum over the entries whose weights it
+// forms and rows 4 grp .. + 3 of every 16-channel tile of O^T.
 template <int D>
 struct Wave8 {
   float m, l;
   f32x4 o[D / 16];
 };
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// x as a sum of three bf16 numbers, two values to a word: the first rounds x, each further one what is left.
+__device__ __forceinline__ void split3(float x0, float x1, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  hi = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x0, x1}, bf16x2));
+  x0 -= __uint_as_float(hi << 16);
+  x1 -= __uint_as_float(hi & 0xffff0000u);
+  mid = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x0, x1}, bf16x2));
+  x0 -= __uint_as_float(mid << 16);
+  x1 -= __uint_as_float(mid & 0xffff0000u);
+  lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x0, x1}, bf16x2));
+}
+
+__device__ __forceinline__ uint32_t row_ror8(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false);
+}
 
 template <typename T, int D, int CODE>
 __device__ __forceinline__ void attend_codes(Wave8<D>& st, const Codes8<D>& x, const Query8<T, D>& q, float scale,
@@ -232,18 +209,19 @@ __device__ __forceinline__ void attend_codes(Wave8<D>& st, const Codes8<D>& x, c
       }
     }
   }
+  // Columns h and h + 8 hold the same head: the first forms the weights of its lane's first eight entries (tiles 0 and
+  // 1), the second those of the others, and they exchange them as bf16 words.
   const float c = scale * x.ks;
-  float mx = kNegInf;
+  float y[8], mx = kNegInf;
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float dot = s[t][r];
-      if constexpr (sizeof(T) == 4) dot += row_ror<8>(dot);   // both parts of the head's query
-      const float y = fmaf(dot, c, has_bias ? x.bias[t][r] : 0.f);
-      s[t][r] = in ? y : kNegInf;
-      mx = fmaxf(mx, s[t][r]);
-    }
+  for (int i = 0; i < 8; ++i) {
+    float dot = low ? s[2 + i / 4][i % 4] : s[i / 4][i % 4];
+    if constexpr (sizeof(T) == 4) dot += row_ror<8>(low ? s[i / 4][i % 4] : s[2 + i / 4][i % 4]);   // the query's parts
+    y[i] = fmaf(dot, c, has_bias ? x.bias[i / 4][i % 4] : 0.f);
+    y[i] = in ? y[i] : kNegInf;
+    mx = fmaxf(mx, y[i]);
+  }
+  mx = fmaxf(mx, row_ror<8>(mx));
   mx = max_xor32(max_xor16(mx));
   const float mnew = fmaxf(st.m, mx);
   const float ref = mnew == kNegInf ? 0.f : mnew;   // nothing unmasked yet: every weight is 0
@@ -254,20 +232,25 @@ __device__ __forceinline__ void attend_codes(Wave8<D>& st, const Codes8<D>& x, c
     for (int i = 0; i < D / 16; ++i) st.o[i] *= corr;
     st.m = mnew;
   }
-  bf16x8 w[2], w_lo[2];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+  for (int i = 0; i < 8; ++i) {
+    y[i] = fast_exp2((y[i] - ref) * kLog2e);
+    st.l += y[i];
+    y[i] *= x.vs;
+  }
+  Chunk16 w0, w1, l0, l1;   // the lane's entries 0 .. 7 and 8 .. 15: head columns the first term, the others the second
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float p = fast_exp2((s[t][r] - ref) * kLog2e);
-      st.l += p;
-      const float y = p * x.vs;
-      const __bf16 hi = (__bf16)y;
-      const float r1 = y - (float)hi;
-      const __bf16 mid = (__bf16)r1;
-      w[t >> 1][(t & 1) * 4 + r] = low ? mid : hi;
-      w_lo[t >> 1][(t & 1) * 4 + r] = low ? (__bf16)0.f : (__bf16)(r1 - (float)mid);
-    }
+  for (int k = 0; k < 4; ++k) {
+    uint32_t hi, mid, lo;
+    split3(y[2 * k], y[2 * k + 1], hi, mid, lo);
+    const uint32_t other = row_ror8(low ? hi : mid), other_lo = row_ror8(lo);
+    w0.w[k] = low ? other : hi;
+    w1.w[k] = low ? mid : other;
+    l0.w[k] = low ? 0u : lo;
+    l1.w[k] = low ? 0u : other_lo;
+  }
+  const bf16x8 w[2] = {__builtin_bit_cast(bf16x8, w0), __builtin_bit_cast(bf16x8, w1)};
+  const bf16x8 w_lo[2] = {__builtin_bit_cast(bf16x8, l0), __builtin_bit_cast(bf16x8, l1)};
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     const bf16x8 v0 = half_to_bf16<CODE, 0>(x.v[i]), v1 = half_to_bf16<CODE, 1>(x.v[i]);
@@ -278,35 +261,140 @@ __device__ __forceinline__ void attend_codes(Wave8<D>& st, const Codes8<D>& x, c
   }
 }
 
-template <typename T, int D, int CODE, bool APP>
-__global__ __launch_bounds__(kThreads, 2) void decode8_kernel(DecodeArgs8 a) {
+// One wave's share of the open block's rows for gn <= kTailG query heads (those at qh): lane group grp takes rows
+// r0 + 4 u + grp, r0 going from `first` by `step`.  rows: those of the block, the appended one (row `fresh`, or -1)
+// last among them.  Leaves the wave's maximum, sum and outputs in LDS.
+template <typename T, int D>
+struct TailRows {
+  static constexpr int U = sizeof(T) == 2 ? 4 : 2;   // rows of a lane group in flight
+  RawSlice<T, D> k[U], v[U];
+  float b[U];
+  __device__ __forceinline__ void load(const char* kt, const char* vt, const char* k_new, const char* v_new,
+                                       const float* bias, int r0, int rows, int fresh, int col, int grp) {
+    constexpr int RB = D * (int)sizeof(T);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = min(r0 + 4 * u + grp, rows - 1);
+      const bool f = r == fresh;
+      k[u].load(f ? k_new : kt + (size_t)r * RB, col);
+      v[u].load(f ? v_new : vt + (size_t)r * RB, col);
+      b[u] = bias && !f ? bias[r] : 0.f;
+    }
+  }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void attend_tail(const char* qh, const char* kt, const char* vt, const char* k_new,
+                                            const char* v_new, const float* bias, int rows, int fresh, float scale,
+                                            int gn, int first, int step, int col, int grp, float* s_m, float* s_l,
+                                            float (*s_o)[D]) {
   constexpr int E = D / 16;
   constexpr int RB = D * (int)sizeof(T);
+  constexpr int U = TailRows<T, D>::U;
+  float q[kTailG][E], m[kTailG], l[kTailG], o[kTailG][E];
+  RawSlice<T, D> qr[kTailG];
+  TailRows<T, D> x;
+  if (first < rows) {   // queries and the first rows in one trip to memory
+#pragma unroll
+    for (int g = 0; g < kTailG; ++g) qr[g].load(qh + (size_t)min(g, gn - 1) * RB, col);
+    x.load(kt, vt, k_new, v_new, bias, first, rows, fresh, col, grp);
+  }
+#pragma unroll
+  for (int g = 0; g < kTailG; ++g) {
+    m[g] = kNegInf;
+    l[g] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      q[g][e] = qr[g].get(e);
+      o[g][e] = 0.f;
+    }
+  }
+  for (int r0 = first; r0 < rows; r0 += step) {
+    bool in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) in[u] = r0 + 4 * u + grp < rows && x.b[u] != kNegInf;
+#pragma unroll
+    for (int g = 0; g < kTailG; ++g) {
+      float y[U], mnew = m[g];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) dot = fmaf(q[g][e], x.k[u].get(e), dot);
+        dot = sum16(dot);
+        y[u] = in[u] ? fmaf(dot, scale, x.b[u]) : kNegInf;
+        mnew = fmaxf(mnew, y[u]);
+      }
+      const float ref = mnew == kNegInf ? 0.f : mnew;
+      const float corr = fast_exp2((m[g] - ref) * kLog2e);
+      m[g] = mnew;
+      l[g] *= corr;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[g][e] *= corr;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float p = fast_exp2((y[u] - ref) * kLog2e);
+        l[g] += p;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[g][e] = in[u] ? fmaf(p, x.v[u].get(e), o[g][e]) : o[g][e];
+      }
+    }
+    if (r0 + step < rows) x.load(kt, vt, k_new, v_new, bias, r0 + step, rows, fresh, col, grp);
+  }
+  // the four lane groups of the wave
+#pragma unroll
+  for (int g = 0; g < kTailG; ++g) {
+    const float M = max_xor32(max_xor16(m[g]));
+    const float c = weight_of(m[g], M);
+    l[g] = add_xor32(add_xor16(l[g] * c));
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[g][e] = add_xor32(add_xor16(o[g][e] * c));
+    if (g < gn && grp == 0) {
+      if (col == 0) {
+        s_m[g] = M;
+        s_l[g] = l[g];
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) s_o[g][col * E + e] = o[g][e];
+    }
+  }
+}
+
+// What a workgroup takes.  Split: four waves over codes or, slot 0, over the tail; the partials go to the workspace.
+// Solo4: the head, tail after codes.  Solo8: the head, four waves over codes and four over the tail side by side.
+enum Role8 { kSplit, kSolo4, kSolo8 };
+
+template <typename T, int D, int CODE, bool APP, Role8 ROLE>
+__global__ __launch_bounds__(ROLE == kSolo8 ? 2 * kThreads : kThreads,
+                                  ROLE != kSolo8 && sizeof(T) == 2 ? 3 : 2) void decode8_kernel(DecodeArgs8 a) {
+  constexpr bool SOLO = ROLE != kSplit;
+  constexpr int NT = ROLE == kSolo8 ? 2 * kThreads : kThreads;
+  constexpr int kParts = SOLO ? 2 * kWaves : kWaves;
+  constexpr int RB = D * (int)sizeof(T);
   // the waves' results over codes, then (where the workgroup takes both) those over the tail
-  __shared__ float s_m[2 * kWaves][kMaxG], s_l[2 * kWaves][kMaxG];
-  __shared__ __align__(16) float s_o[2 * kWaves][kMaxG][D];
+  __shared__ float s_m[kParts][kMaxG], s_l[kParts][kMaxG];
+  __shared__ __align__(16) float s_o[kParts][kMaxG][D];
   __shared__ float s_max[4];
-  const int64_t head = blockIdx.y;
+  const uint32_t head = blockIdx.y;
   const int slot = blockIdx.x, G = a.G;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
-  const int block = a.c.block, cap = a.c.capacity;
-  const int len = entries_of(a.n, (int)(head / a.hkv));
+  const int shift = a.block_shift, block = 1 << shift, cap = a.c.capacity;
+  const int len = a.n.lens ? min(a.n.lens[head / (uint32_t)a.hkv], a.n.cache_len) : a.n.cache_len;
   const bool active = len >= 0;
-  const int whole = active ? len / block * block : 0;    // entries held as codes
+  const int whole = active ? len >> shift << shift : 0;  // entries held as codes
   const int rest = active ? len - whole : 0;             // rows in the tail
-  const bool solo = a.slots == 1;
-  const bool codes_here = slot < a.nsplit, tail_here = solo || slot == a.nsplit;
+  const bool codes_here = ROLE == kSolo8 ? wave < kWaves : SOLO || slot > 0;
+  const bool tail_here = ROLE == kSolo8 ? wave >= kWaves : SOLO || slot == 0;
   const float* bh = a.bias ? a.bias + (size_t)head * cap : nullptr;
   const char* qh = a.q + (size_t)head * G * RB;
 
   if (codes_here) {
-    const int groups = (whole + kGroup - 1) / kGroup;
-    const int e0 = (int)((int64_t)groups * slot / a.nsplit) * kGroup;
-    const int e1 = min((int)((int64_t)groups * (slot + 1) / a.nsplit) * kGroup, whole);
+    const int e0 = SOLO ? 0 : (slot - 1) * a.chunk;
+    const int e1 = SOLO ? whole : min(e0 + a.chunk, whole);
+    if (!SOLO && e0 >= e1) return;   // behind a shorter sequence's end: the combining kernel does not read the slot
     const char* Kh = a.c.K + (size_t)head * cap * D;
     const char* Vh = a.c.V + (size_t)head * cap * D;
-    const int shift = 31 - __builtin_clz(block);
     const float* ks = a.c.k_scale + (size_t)head * (cap >> shift);
     const float* vs = a.c.v_scale + (size_t)head * (cap >> shift);
     Query8<T, D> q;
@@ -321,6 +409,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(DecodeArgs8 a) {
       load_codes<D>(x, Kh, Vh, ks, vs, bh, shift, e, e1, col, grp);
       attend_codes<T, D, CODE>(st, x, q, a.scale, bh != nullptr, e + 16 * grp < e1, col >= 8);
     }
+    st.l += row_ror<8>(st.l);
     st.l = add_xor32(add_xor16(st.l));
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
@@ -335,61 +424,31 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(DecodeArgs8 a) {
     }
   }
   if (tail_here) {
-    float q[kMaxG][E];
-#pragma unroll
-    for (int g = 0; g < kMaxG; ++g)
-      if (g < G) load_row<T, D>(qh + (size_t)g * RB, col, q[g]);
-    State8<E> s;
-    s.clear();
-    const char* kt = a.c.k_tail + (size_t)head * block * RB;
-    const char* vt = a.c.v_tail + (size_t)head * block * RB;
-    const int rows = active ? rest + (APP ? 1 : 0) : 0;
-    for (int r0 = wave * 4; r0 < rows; r0 += kWaves * 4) {
-      const int r = min(r0 + grp, rows - 1);
-      const bool fresh = APP && r == rest;
-      float k[E], v[E];
-      load_row<T, D>(fresh ? a.k_new + (size_t)head * RB : kt + (size_t)r * RB, col, k);
-      load_row<T, D>(fresh ? a.v_new + (size_t)head * RB : vt + (size_t)r * RB, col, v);
-      const float b = bh && !fresh ? bh[whole + r] : 0.f;
-      attend<E>(s, q, G, k, v, a.scale, b, r0 + grp < rows && b != kNegInf);
-    }
-    // the four lane groups of a wave
-    const int at = codes_here ? kWaves + wave : wave;
-#pragma unroll
-    for (int g = 0; g < kMaxG; ++g) {
-      if (g >= G) break;
-#pragma unroll
-      for (int off = 16; off <= 32; off <<= 1) {
-        const float m2 = xor_shfl(s.m[g], off), l2 = xor_shfl(s.l[g], off);
-        const float M = fmaxf(s.m[g], m2);
-        const float c1 = weight_of(s.m[g], M), c2 = weight_of(m2, M);
-        s.l[g] = s.l[g] * c1 + l2 * c2;
-#pragma unroll
-        for (int e = 0; e < E; ++e) s.o[g][e] = s.o[g][e] * c1 + xor_shfl(s.o[g][e], off) * c2;
-        s.m[g] = M;
-      }
-      if (grp == 0) {
-        if (col == 0) {
-          s_m[at][g] = s.m[g];
-          s_l[at][g] = s.l[g];
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) s_o[at][g][col * E + e] = s.o[g][e];
-      }
-    }
+    // with more than kTailG query heads half of the waves take the rest of them
+    const int w = wave % kWaves, half = G > kTailG ? 2 : 1, g0 = w / (kWaves / half) * kTailG;
+    const int at = SOLO ? kWaves + w : w;
+    const int per_wave = 4 * TailRows<T, D>::U;
+    const size_t row0 = (size_t)head << shift;
+    if (lane < kMaxG) s_m[at][lane] = kNegInf;   // of the heads that the wave does not take
+    attend_tail<T, D>(qh + (size_t)g0 * RB, a.c.k_tail + row0 * RB, a.c.v_tail + row0 * RB,
+                      APP ? a.k_new + (size_t)head * RB : nullptr, APP ? a.v_new + (size_t)head * RB : nullptr,
+                      bh ? bh + whole : nullptr, active ? rest + (APP ? 1 : 0) : 0, APP ? rest : -1, a.scale,
+                      min(G - g0, kTailG), w % (kWaves / half) * per_wave, kWaves / half * per_wave, col, grp,
+                      &s_m[at][g0], &s_l[at][g0], &s_o[at][g0]);
   }
   __syncthreads();
-  const int parts = solo ? 2 * kWaves : kWaves;
-  for (int idx = threadIdx.x; idx < G * D; idx += kThreads) {
+  for (int idx = threadIdx.x; idx < G * D; idx += NT) {
     const int g = idx / D, dd = idx % D;
     float M = kNegInf, l = 0.f, o = 0.f;
-    for (int w = 0; w < parts; ++w) M = fmaxf(M, s_m[w][g]);
-    for (int w = 0; w < parts; ++w) {
+#pragma unroll
+    for (int w = 0; w < kParts; ++w) M = fmaxf(M, s_m[w][g]);
+#pragma unroll
+    for (int w = 0; w < kParts; ++w) {
       const float c = weight_of(s_m[w][g], M);
-      l = fmaf(s_l[w][g], c, l);
-      o = fmaf(s_o[w][g][dd], c, o);
+      l = c > 0.f ? fmaf(s_l[w][g], c, l) : l;       // a part without entries may hold anything
+      o = c > 0.f ? fmaf(s_o[w][g][dd], c, o) : o;
     }
-    if (solo) {
+    if (SOLO) {
       a.out[(size_t)head * G * D + idx] = l > 0.f ? o / l : 0.f;
     } else {
       a.part_o[((size_t)head * a.slots + slot) * G * D + idx] = o;
@@ -399,7 +458,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(DecodeArgs8 a) {
 
   // the appended token: its row into the tail, the bias 0, and the block it completes into codes.  Nothing else in the
   // launch reads what is written here.
-  if (APP && tail_here && active) {
+  if (APP && (SOLO || slot == 0) && active) {
     char* kt = a.c.k_tail + (size_t)head * block * RB;
     char* vt = a.c.v_tail + (size_t)head * block * RB;
     const char* kn = a.k_new + (size_t)head * RB;
@@ -412,7 +471,7 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(DecodeArgs8 a) {
     if (rest + 1 == block) {
       const BlockThread bt = block_thread<D>(threadIdx.x, block);
       const int byte = bt.c4 * 4 * (int)sizeof(T);
-      const size_t entry = (size_t)head * cap + whole, blk = (size_t)head * (cap / block) + whole / block;
+      const size_t entry = (size_t)head * cap + whole, blk = (size_t)head * (cap >> shift) + (whole >> shift);
       for (int v = 0; v < 2; ++v) {
         const char* t = v ? vt : kt;
         const char* n = v ? vn : kn;
@@ -428,71 +487,108 @@ __global__ __launch_bounds__(kThreads, 2) void decode8_kernel(DecodeArgs8 a) {
   }
 }
 
-// Combines the partials of a head in slot order: one workgroup per query head, thread (dd, sub) takes the slots sub,
-// sub + S, ... of output channel dd, the S runs then meet in LDS.
-template <int D>
-__global__ __launch_bounds__(256) void decode8_reduce_kernel(const float* part_o, const float2* part_ml, float* out,
-                                                             int slots, int G) {
-  constexpr int S = 256 / D;
-  constexpr int kBatch = 8;
-  __shared__ float s_m[S], s_l[S], s_o[S][D];
-  const int64_t head = blockIdx.x;
-  const int g = blockIdx.y, dd = threadIdx.x % D, sub = threadIdx.x / D;
-  const float2* ml = part_ml + (size_t)head * slots * G + g;
-  const float* po = part_o + ((size_t)head * slots * G + g) * D + dd;
-  float m = kNegInf, l = 0.f, o = 0.f;
-  for (int s0 = sub; s0 < slots; s0 += S * kBatch) {
-    float ov[kBatch];
+// Combines the partials of the query heads, in slot order.  A unit of d/4 threads takes four channels each of the
+// slots sub, sub + SUB, ... of a query head and loads kBatch of them at a time; with SUB > 1 the runs then meet in
+// LDS, in order.  SUB = 1 where a head has few slots (a unit then has them all in flight at once), otherwise the
+// whole workgroup takes one query head: 100 slots in one trip to memory.
+template <int D, int SUB>
+__global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int qheads) {
+  constexpr int kUnits = 256 / (D / 4);   // 8 or 16
+  constexpr int kBatch = D == 128 || SUB == 1 ? 16 : 8;
+  static_assert(SUB == 1 || SUB == kUnits, "a unit is a query head, or all of them are one");
+  __shared__ float s_m[kUnits], s_l[kUnits];
+  __shared__ __align__(16) float s_o[kUnits][D];
+  const int c4 = threadIdx.x % (D / 4), unit = threadIdx.x / (D / 4), sub = SUB == 1 ? 0 : unit;
+  const uint32_t qh = SUB == 1 ? min(blockIdx.x * kUnits + unit, (uint32_t)qheads - 1) : blockIdx.x;
+  const uint32_t head = qh / (uint32_t)a.G, g = qh % (uint32_t)a.G;
+  const int len = a.n.lens ? min(a.n.lens[head / (uint32_t)a.hkv], a.n.cache_len) : a.n.cache_len;
+  const int whole = len > 0 ? len >> a.block_shift << a.block_shift : 0;
+  const int slots = 1 + (whole + a.chunk - 1) / a.chunk;    // those of the splits that had entries
+  const float2* ml = a.part_ml + (size_t)head * a.slots * a.G + g;
+  const float* po = a.part_o + ((size_t)head * a.slots * a.G + g) * D + c4 * 4;
+  float m = kNegInf, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < slots; s0 += SUB * kBatch) {
+    f32x4 ov[kBatch];
     float2 v[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const int sl = min(s0 + u * S, slots - 1);
-      ov[u] = po[(size_t)sl * G * D];
-      v[u] = ml[(size_t)sl * G];
-      if (s0 + u * S >= slots) v[u].x = kNegInf;
+      if (s0 + u * SUB < slots) {
+        const int sl = min(s0 + u * SUB + sub, slots - 1);
+        ov[u] = *reinterpret_cast<const f32x4*>(po + (size_t)sl * a.G * D);
+        v[u] = ml[(size_t)sl * a.G];
+      }
     }
     float M = m;
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) M = fmaxf(M, v[u].x);
+    for (int u = 0; u < kBatch; ++u) {
+      if (s0 + u * SUB + sub >= slots) {
+        v[u] = make_float2(kNegInf, 0.f);
+        ov[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      M = fmaxf(M, v[u].x);
+    }
     const float c = weight_of(m, M);
     l *= c;
     o *= c;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const float w = weight_of(v[u].x, M);
-      l = fmaf(v[u].y, w, l);
-      o = fmaf(ov[u], w, o);
+      if (s0 + u * SUB < slots) {
+        const float w = weight_of(v[u].x, M);
+        l = fmaf(v[u].y, w, l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(ov[u][e], w, o[e]);
+      }
     }
     m = M;
   }
-  s_o[sub][dd] = o;
-  if (dd == 0) {
-    s_m[sub] = m;
-    s_l[sub] = l;
-  }
-  __syncthreads();
-  if (sub == 0) {
-    float M = kNegInf, L = 0.f, t = 0.f;
-#pragma unroll
-    for (int k = 0; k < S; ++k) M = fmaxf(M, s_m[k]);
-#pragma unroll
-    for (int k = 0; k < S; ++k) {
-      const float w = weight_of(s_m[k], M);
-      t = fmaf(s_o[k][dd], w, t);
-      L = fmaf(s_l[k], w, L);
+  if constexpr (SUB == 1) {
+    const float inv = 1.f / l;
+    if (blockIdx.x * kUnits + unit < (uint32_t)qheads)
+      *reinterpret_cast<f32x4*>(a.out + (size_t)qh * D + c4 * 4) = l > 0.f ? o * inv : f32x4{0.f, 0.f, 0.f, 0.f};
+  } else {
+    *reinterpret_cast<f32x4*>(&s_o[unit][c4 * 4]) = o;
+    if (c4 == 0) {
+      s_m[unit] = m;
+      s_l[unit] = l;
     }
-    out[((size_t)head * G + g) * D + dd] = L > 0.f ? t / L : 0.f;
+    __syncthreads();
+    for (int dd = threadIdx.x; dd < D; dd += 256) {
+      float M = kNegInf, L = 0.f, t = 0.f;
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k) M = fmaxf(M, s_m[k]);
+#pragma unroll
+      for (int k = 0; k < kUnits; ++k) {
+        const float w = weight_of(s_m[k], M);
+        t = fmaf(s_o[k][dd], w, t);
+        L = fmaf(s_l[k], w, L);
+      }
+      a.out[(size_t)qh * D + dd] = L > 0.f ? t / L : 0.f;
+    }
   }
+}
+
+template <typename T, int D, int CODE, Role8 ROLE>
+void launch_role(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
+  const dim3 grid(a.slots, (unsigned)heads), blk(ROLE == kSolo8 ? 2 * kThreads : kThreads);
+  if (a.k_new) hipLaunchKernelGGL((decode8_kernel<T, D, CODE, true, ROLE>), grid, blk, 0, st, a);
+  else hipLaunchKernelGGL((decode8_kernel<T, D, CODE, false, ROLE>), grid, blk, 0, st, a);
 }
 
 template <typename T, int D, int CODE>
 hipError_t launch_tdc(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
-  const dim3 grid(a.slots, (unsigned)heads);
-  if (a.k_new) hipLaunchKernelGGL((decode8_kernel<T, D, CODE, true>), grid, dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((decode8_kernel<T, D, CODE, false>), grid, dim3(kThreads), 0, st, a);
-  if (a.slots > 1)
-    hipLaunchKernelGGL((decode8_reduce_kernel<D>), dim3((unsigned)heads, a.G), dim3(256), 0, st, a.part_o, a.part_ml,
-                       a.out, a.slots, a.G);
+  if (a.slots == 1) {
+    if (a.n.cache_len <= kSolo8Entries) launch_role<T, D, CODE, kSolo8>(heads, a, st);
+    else launch_role<T, D, CODE, kSolo4>(heads, a, st);
+    return hipGetLastError();
+  }
+  launch_role<T, D, CODE, kSplit>(heads, a, st);
+  constexpr int kUnits = 256 / (D / 4);
+  const int qheads = (int)heads * a.G;
+  if (a.slots <= kFewSlots)
+    hipLaunchKernelGGL((decode8_reduce_kernel<D, 1>), dim3((qheads + kUnits - 1) / kUnits), dim3(256), 0, st, a, qheads);
+  else
+    hipLaunchKernelGGL((decode8_reduce_kernel<D, kUnits>), dim3(qheads), dim3(256), 0, st, a, qheads);
   return hipGetLastError();
 }
 
@@ -501,22 +597,40 @@ hipError_t launch_td(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
   return a.c.code == SELKV_I8 ? launch_tdc<T, D, SELKV_I8>(heads, a, st) : launch_tdc<T, D, SELKV_E4M3>(heads, a, st);
 }
 
+// Splits of one head: whole rounds of the four waves' groups, as many as fill the chip when every sequence has
+// cache_len entries, three times as many where the sequences have lengths of their own.
+int64_t most_splits(int64_t heads, int64_t groups, bool ragged) {
+  const int64_t target = (ragged ? 3 : 1) * kTargetBlocks;
+  return std::max<int64_t>(1, std::min({(target + heads - 1) / heads, (groups + kWaves - 1) / kWaves, (int64_t)kMaxSplit}));
+}
+
+size_t partial_bytes(int64_t heads, int64_t slots, int d, int G, size_t* ml) {
+  *ml = ((size_t)heads * slots * G * sizeof(float2) + 255) & ~(size_t)255;
+  return *ml + (((size_t)heads * slots * G * d * sizeof(float) + 255) & ~(size_t)255);
+}
+
 }  // namespace
 
-// The number of splits grows with cache_len, so a workspace for the capacity serves every length.
-Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G) {
+Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G, bool ragged) {
   Decode8Plan p{};
   const int64_t groups = ((int64_t)cache_len + kGroup - 1) / kGroup;
-  int64_t nsplit = (kTargetBlocks + heads - 1) / heads;
-  if (nsplit > (groups + 3) / 4) nsplit = (groups + 3) / 4;
-  if (nsplit > kMaxSplit) nsplit = kMaxSplit;
-  if (nsplit < 1) nsplit = 1;
-  p.nsplit = (int)nsplit;
-  p.slots = nsplit == 1 ? 1 : (int)nsplit + 1;
-  if (p.slots == 1) return p;
-  p.ml_bytes = ((size_t)heads * p.slots * G * sizeof(float2) + 255) & ~(size_t)255;
-  p.bytes = p.ml_bytes + (((size_t)heads * p.slots * G * d * sizeof(float) + 255) & ~(size_t)255);
+  const int64_t most = most_splits(heads, groups, ragged);
+  p.slots = 1;
+  if (cache_len <= kSolo8Entries || most == 1) return p;
+  int64_t per = (groups + most - 1) / most;          // groups of a split
+  per = (per + kWaves - 1) / kWaves * kWaves;
+  p.chunk = (int)(per * kGroup);
+  p.slots = (int)((groups + per - 1) / per) + 1;
+  p.bytes = partial_bytes(heads, p.slots, d, G, &p.ml_bytes);
   return p;
+}
+
+// Covers plan_decode8 at every length up to the capacity: its splits are at most most_splits(), which grows with it.
+size_t decode8_workspace_bound(int64_t heads, int capacity, int d, int G) {
+  size_t ml;
+  const int64_t groups = ((int64_t)capacity + kGroup - 1) / kGroup;
+  const int64_t most = most_splits(heads, groups, true);
+  return capacity <= kSolo8Entries || most == 1 ? 0 : partial_bytes(heads, most + 1, d, G, &ml);
 }
 
 hipError_t launch_decode8(int64_t heads, int hkv, int d, int G, int dtype, float scale, const Decode8Plan& p,
@@ -534,8 +648,9 @@ hipError_t launch_decode8(int64_t heads, int hkv, int d, int G, int dtype, float
   a.v_new = static_cast<const char*>(v_new);
   a.hkv = hkv;
   a.G = G;
-  a.nsplit = p.nsplit;
   a.slots = p.slots;
+  a.chunk = p.chunk;
+  a.block_shift = 31 - __builtin_clz((unsigned)c.block);
   a.scale = scale;
   if (dtype == SELKV_BF16) return d == 128 ? launch_td<bf16_t, 128>(heads, a, st) : launch_td<bf16_t, 64>(heads, a, st);
   return d == 128 ? launch_td<float, 128>(heads, a, st) : launch_td<float, 64>(heads, a, st);

@@ -139,13 +139,14 @@ struct Lens8 {
 };
 
 struct Decode8Plan {
-  int nsplit;          // workgroups per KV head over the codes (1: one workgroup takes the head, tail included)
-  int slots;           // partials per KV head
+  int chunk;           // entries of a split
+  int slots;           // partials per KV head: the tail's and one per split (1: one workgroup takes the head)
   size_t ml_bytes;     // (max, sum) partials, at the start of the workspace
   size_t bytes;
 };
 
-Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G);
+Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G, bool ragged);   // ragged: lengths of their own
+size_t decode8_workspace_bound(int64_t heads, int capacity, int d, int G);
 
 hipError_t launch_cache8_write(int64_t heads, int hkv, int d, int dtype, const Cache8& c, const Lens8& n,
                                const int32_t* counts, const void* K_new, const void* V_new, int n_new, hipStream_t st);

@@ -524,7 +524,7 @@ SELKV_API selkv_status selkv_decode8_workspace_size(const selkv_params* p, const
   if (st != SELKV_OK) return st;
   if (p->group < 1) return SELKV_EINVAL;
   if (p->group > 8) return SELKV_EUNSUPPORTED;
-  *bytes = plan_decode8((int64_t)p->batch * p->n_heads_kv, c->capacity, p->head_dim, p->group).bytes;
+  *bytes = decode8_workspace_bound((int64_t)p->batch * p->n_heads_kv, c->capacity, p->head_dim, p->group);
   return SELKV_OK;
 }
 
@@ -534,7 +534,7 @@ SELKV_API selkv_status selkv_decode8_attn(const selkv_params* p, const selkv_cac
   selkv_status st = check_decode8(p, c, q, bias, cache_len, lens, out);
   if (st != SELKV_OK) return st;
   const int64_t heads = (int64_t)p->batch * p->n_heads_kv;
-  const Decode8Plan plan = plan_decode8(heads, cache_len, p->head_dim, p->group);
+  const Decode8Plan plan = plan_decode8(heads, cache_len, p->head_dim, p->group, lens != nullptr);
   if ((st = check_ws(ws, ws_bytes, plan.bytes)) != SELKV_OK) return st;
   return hip_status(launch_decode8(heads, p->n_heads_kv, p->head_dim, p->group, p->kv_dtype, eff_scale(p), plan,
                                    view_cache8(c), Lens8{cache_len, lens}, q, const_cast<float*>(bias), nullptr,
@@ -551,7 +551,7 @@ SELKV_API selkv_status selkv_decode8_append(const selkv_params* p, const selkv_c
   if (!k_new || !v_new) return SELKV_EINVAL;
   if (!aligned(k_new, 16) || !aligned(v_new, 16)) return SELKV_EALIGN;
   const int64_t heads = (int64_t)p->batch * p->n_heads_kv;
-  const Decode8Plan plan = plan_decode8(heads, cache_len, p->head_dim, p->group);
+  const Decode8Plan plan = plan_decode8(heads, cache_len, p->head_dim, p->group, lens != nullptr);
   if ((st = check_ws(ws, ws_bytes, plan.bytes)) != SELKV_OK) return st;
   return hip_status(launch_decode8(heads, p->n_heads_kv, p->head_dim, p->group, p->kv_dtype, eff_scale(p), plan,
                                    view_cache8(c), Lens8{cache_len, lens}, q, bias, k_new, v_new, out, ws, stream));
