@@ -3,13 +3,18 @@
 //
 // Write: a workgroup of 256 threads takes whole blocks (1 .. 16 of them, by
 // their size).  A block is read once, its rows stay in registers while the
-// largest magnitude is found, and its codes are stored: d * sizeof(T) bytes
-// read and d written per row, with no scratch and one launch for K and V.
+// largest magnitude is found, and its codes meet in LDS in the order of the
+// cache, to be stored line by line: d * sizeof(T) bytes read and d written per
+// row, with no scratch and one launch for K and V.
 // The rows of the first block may lie in the tail (the open block of earlier
 // calls); the workgroup that reads them there is the one that later overwrites
 // the tail with the call's own incomplete block, behind a barrier.
 // Read: a thread takes 16 tokens x 4 channels, as the write does.
-// Both are bound by the memory they move.
+// Both are bound by the memory they move.  Stores pass the caches' replacement
+// order by (nothing here is read again): 32 layers x 8 heads x 25600 rows of
+// bf16 are written in 909 us, 5.5 TB/s, against 926 with ordinary stores and 968
+// with each thread's codes stored as it holds them (16-byte pieces 64 bytes
+// apart); a layer of them is read back in 24.9 us, 6.3 TB/s, against 33.9.
 #include "cache8.hpp"
 
 namespace selkv {
@@ -30,6 +35,7 @@ template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void cache8_write_kernel(WriteArgs a) {
   constexpr int RB = D * (int)sizeof(T);
   __shared__ float s_max[4];
+  __shared__ __align__(16) char s_codes[kThreads * 64];   // the workgroup's codes, as they lie in the cache
   const bool is_v = blockIdx.z != 0;
   const int64_t head = blockIdx.y;
   const int b = (int)(head / a.hkv);
@@ -51,15 +57,23 @@ __global__ __launch_bounds__(kThreads) void cache8_write_kernel(WriteArgs a) {
     const int i_blk = blockIdx.x * per_wg + bt.sub;
     const int rel0 = i_blk * block + bt.tile * 16;   // the thread's first token, counted from block fb's first
     const int byte = bt.c4 * 4 * (int)sizeof(T);
-    const size_t entry = (size_t)head * cap + (size_t)(fb + i_blk) * block;   // K and V: d bytes per entry
     quantise_blocks<T, D, CODE>(
         i_blk < full, bt, block, is_v,
         [&](int i) {
           const int rel = rel0 + i;
           return (rel < r0 ? tail + (size_t)rel * RB : fresh + (size_t)(rel - r0) * RB) + byte;
         },
-        (is_v ? a.c.V : a.c.K) + entry * D, (is_v ? a.c.v_scale : a.c.k_scale) + (size_t)head * (cap / block) + fb + i_blk,
+        s_codes + (size_t)bt.sub * block * D, (is_v ? a.c.v_scale : a.c.k_scale) + (size_t)head * (cap / block) + fb + i_blk,
         s_max);
+    __syncthreads();
+    const int first = blockIdx.x * per_wg;
+    char* to = (is_v ? a.c.V : a.c.K) + ((size_t)head * cap + (size_t)(fb + first) * block) * D;
+    const int bytes = min(per_wg, full - first) * block * D;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int at = (s * kThreads + (int)threadIdx.x) * 16;
+      if (at < bytes) store16_streaming(to + at, load16(s_codes + at));
+    }
   }
   if (blockIdx.x > 0) return;
   // the rows of the last, incomplete block: behind those that the tail holds, or from its start
@@ -132,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void cache8_read_kernel(ReadArgs a) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int e = t0 + i;
-    if (e >= a.first && e < end) x[i].store(out + (size_t)(e - a.first) * RB);
+    if (e >= a.first && e < end) x[i].store_streaming(out + (size_t)(e - a.first) * RB);
   }
 }
 

@@ -25,12 +25,18 @@ __device__ __forceinline__ int entries_of(const Lens8& n, int b) {
   return n.lens ? min(n.lens[b], n.cache_len) : n.cache_len;
 }
 
-// Four elements of a row in storage type T, raw.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Four elements of a row in storage type T, raw.  store_streaming: past the caches' replacement order, for rows that
+// the call does not read again and that whole wavefronts write line by line.
 template <typename T> struct Quad;
 template <> struct Quad<float> {
   uint4 w;
   __device__ __forceinline__ void load(const char* p) { w = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void store(char* p) const { *reinterpret_cast<uint4*>(p) = w; }
+  __device__ __forceinline__ void store_streaming(char* p) const {
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), reinterpret_cast<u32x4*>(p));
+  }
   __device__ __forceinline__ float get(int e) const {
     return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w);
   }
@@ -41,7 +47,9 @@ template <> struct Quad<float> {
 template <> struct Quad<bf16_t> {
   uint2 w;
   __device__ __forceinline__ void load(const char* p) { w = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void store(char* p) const { *reinterpret_cast<uint2*>(p) = w; }
+  __device__ __forceinline__ void store_streaming(char* p) const {
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x2, w), reinterpret_cast<u32x2*>(p));
+  }
   __device__ __forceinline__ float get(int e) const {
     const uint32_t x = e < 2 ? w.x : w.y;
     return __uint_as_float((e & 1) ? (x & 0xffff0000u) : (x << 16));
@@ -51,6 +59,10 @@ template <> struct Quad<bf16_t> {
     w.y = f32_to_bf16(x[2]) | ((uint32_t)f32_to_bf16(x[3]) << 16);
   }
 };
+
+__device__ __forceinline__ void store16_streaming(char* p, const Chunk16& c) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, c), reinterpret_cast<u32x4*>(p));
+}
 
 // |x|, or 0 for an infinity or a NaN.
 __device__ __forceinline__ float finite_abs(float x) {
@@ -100,8 +112,8 @@ __device__ __forceinline__ void decode4(uint32_t w, float (&x)[4]) {
 // its channels, so V's tiles need no exchange between threads.  Per block
 // block/16 * d/4 = 16 .. 256 threads.  Every thread of the workgroup calls it
 // (it has barriers); `on`: the thread has a block.
-// row(i): address of the thread's channels in token i of its tile; codes,
-// scale: of the thread's block (codes at its first entry).
+// row(i): address of the thread's channels in token i of its tile; codes (in
+// the cache, or LDS to be copied there), scale: of the thread's block.
 struct BlockThread {
   int sub, tile, c4;   // block among those of the workgroup, 16-token tile in it, channel / 4
 };

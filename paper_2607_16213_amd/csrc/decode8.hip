@@ -43,7 +43,7 @@ constexpr int kTailG = 4;             // query heads of a pass over the tail: re
 constexpr int kGroup = 64;            // entries of a wave's step; splits are whole multiples of them
 constexpr int kTargetBlocks = 768;    // workgroups that a launch aims at: three to a CU, what its registers hold
 constexpr int kMaxSplit = 512;
-constexpr int kSolo8Entries = 512;    // up to them a workgroup takes a head by itself
+constexpr int kSolo8Entries = 768;    // up to them a workgroup takes a head by itself
 constexpr int kFewSlots = 16;
 
 struct DecodeArgs8 {
