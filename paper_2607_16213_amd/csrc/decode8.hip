@@ -41,9 +41,13 @@ constexpr int kThreads = kWaves * 64;
 constexpr int kMaxG = 8;
 constexpr int kTailG = 4;             // query heads of a pass over the tail: registers, shared with the codes' loop
 constexpr int kGroup = 64;            // entries of a wave's step; splits are whole multiples of them
-constexpr int kTargetBlocks = 768;    // workgroups that a launch aims at: three to a CU, what its registers hold
+constexpr int kTargetBlocks = 768;    // a round of workgroups: three to a CU, what its registers hold
+constexpr int kRounds = 3;
 constexpr int kMaxSplit = 512;
-constexpr int kSolo8Entries = 768;    // up to them a workgroup takes a head by itself
+// up to them a workgroup takes a head by itself: at 8 heads 700 entries take 9.9 us so and 10.4 in splits with the
+// second kernel, 900 entries 11.8 and 10.4
+constexpr int kSoloEntries = 768;
+constexpr int kCUs = 256;
 constexpr int kFewSlots = 16;
 
 struct DecodeArgs8 {
@@ -56,9 +60,19 @@ struct DecodeArgs8 {
   float2* part_ml;   // [heads, slots, G]
   const char* k_new; // APP
   const char* v_new;
-  int hkv, G, slots, chunk, block_shift;   // chunk: entries of a split
+  int hkv, G, slots, block_shift;
+  int chunk;         // entries of a split where every sequence has cache_len
   float scale;
 };
+
+// Entries of a split of a sequence whose codes are `whole` entries: with lengths of their own each is cut into as many
+// splits as its slots allow, whole steps of the four waves, so a bound far above the lengths costs no parallelism.
+__device__ __forceinline__ int chunk_of(const DecodeArgs8& a, int whole) {
+  if (!a.n.lens) return a.chunk;
+  const uint32_t splits = a.slots - 1, step = kWaves * kGroup;
+  const uint32_t per = ((uint32_t)whole + splits - 1) / splits;
+  return (int)(max((per + step - 1) / step, 1u) * step);
+}
 
 // Weight of partial (m, .) against the maximum M of all (0 where it is empty).
 __device__ __forceinline__ float weight_of(float m, float M) {
@@ -390,8 +404,9 @@ __global__ __launch_bounds__(ROLE == kSolo8 ? 2 * kThreads : kThreads,
   const char* qh = a.q + (size_t)head * G * RB;
 
   if (codes_here) {
-    const int e0 = SOLO ? 0 : (slot - 1) * a.chunk;
-    const int e1 = SOLO ? whole : min(e0 + a.chunk, whole);
+    const int chunk = SOLO ? whole : chunk_of(a, whole);
+    const int e0 = SOLO ? 0 : (slot - 1) * chunk;
+    const int e1 = min(e0 + chunk, whole);
     if (!SOLO && e0 >= e1) return;   // behind a shorter sequence's end: the combining kernel does not read the slot
     const char* Kh = a.c.K + (size_t)head * cap * D;
     const char* Vh = a.c.V + (size_t)head * cap * D;
@@ -503,7 +518,8 @@ __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int 
   const uint32_t head = qh / (uint32_t)a.G, g = qh % (uint32_t)a.G;
   const int len = a.n.lens ? min(a.n.lens[head / (uint32_t)a.hkv], a.n.cache_len) : a.n.cache_len;
   const int whole = len > 0 ? len >> a.block_shift << a.block_shift : 0;
-  const int slots = 1 + (whole + a.chunk - 1) / a.chunk;    // those of the splits that had entries
+  const int chunk = chunk_of(a, whole);
+  const int slots = 1 + (whole + chunk - 1) / chunk;    // the tail's and those of the splits that had entries
   const float2* ml = a.part_ml + (size_t)head * a.slots * a.G + g;
   const float* po = a.part_o + ((size_t)head * a.slots * a.G + g) * D + c4 * 4;
   float m = kNegInf, l = 0.f;
@@ -578,7 +594,9 @@ void launch_role(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
 template <typename T, int D, int CODE>
 hipError_t launch_tdc(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
   if (a.slots == 1) {
-    if (a.n.cache_len <= kSolo8Entries) launch_role<T, D, CODE, kSolo8>(heads, a, st);
+    // eight waves where every head has a CU to itself: with more of them four idle ones cost too much (64 x 8 heads
+    // of 300 entries: 15.2 us in four waves each, 17.2 in eight; 32 x 8 heads: 10.9 and 9.3)
+    if (heads <= kCUs) launch_role<T, D, CODE, kSolo8>(heads, a, st);
     else launch_role<T, D, CODE, kSolo4>(heads, a, st);
     return hipGetLastError();
   }
@@ -597,11 +615,17 @@ hipError_t launch_td(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
   return a.c.code == SELKV_I8 ? launch_tdc<T, D, SELKV_I8>(heads, a, st) : launch_tdc<T, D, SELKV_E4M3>(heads, a, st);
 }
 
-// Splits of one head: whole rounds of the four waves' groups, as many as fill the chip when every sequence has
-// cache_len entries, three times as many where the sequences have lengths of their own.
-int64_t most_splits(int64_t heads, int64_t groups, bool ragged) {
-  const int64_t target = (ragged ? 3 : 1) * kTargetBlocks;
-  return std::max<int64_t>(1, std::min({(target + heads - 1) / heads, (groups + kWaves - 1) / kWaves, (int64_t)kMaxSplit}));
+// Most splits of one head: those that give the chip kRounds rounds of workgroups, none shorter than one step of its
+// four waves; none where the heads alone are a round.
+int64_t most_splits(int64_t heads, int64_t groups) {
+  if (heads >= kTargetBlocks) return 1;
+  return std::max<int64_t>(1, std::min({(kRounds * kTargetBlocks + heads - 1) / heads, (groups + kWaves - 1) / kWaves,
+                                        (int64_t)kMaxSplit}));
+}
+
+// Groups of a split where a head of `groups` is to have about `want` of them: whole steps of the four waves.
+int64_t split_groups(int64_t groups, int64_t want) {
+  return ((groups + want - 1) / want + kWaves - 1) / kWaves * kWaves;
 }
 
 size_t partial_bytes(int64_t heads, int64_t slots, int d, int G, size_t* ml) {
@@ -611,16 +635,28 @@ size_t partial_bytes(int64_t heads, int64_t slots, int d, int G, size_t* ml) {
 
 }  // namespace
 
+// Splits.  Three rounds of workgroups let fast ones make up for slow ones and for sequences of other lengths: 4 x 32
+// heads of 4096 entries take 29.6 us in 2048 workgroups, 32.3 in 768 (and 35.8 in 512); a ragged batch of 16 x 8 heads
+// of 0 - 8100 entries 34.7 us, 44.1 in 768.  (A sequence of its own length is cut anew on the device, chunk_of.)
+// Every workgroup costs its prologue and its partials, though, so one round is taken where it comes out even: 32 x 8
+// heads of 25641 entries take 299 us in 768 workgroups, 312 in 2304; and a round that is barely exceeded is not begun:
+// 8 heads of 25600 entries take 16.2 us in 400 workgroups, 17.1 in 800.
 Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G, bool ragged) {
   Decode8Plan p{};
   const int64_t groups = ((int64_t)cache_len + kGroup - 1) / kGroup;
-  const int64_t most = most_splits(heads, groups, ragged);
+  const int64_t most = most_splits(heads, groups);
   p.slots = 1;
-  if (cache_len <= kSolo8Entries || most == 1) return p;
-  int64_t per = (groups + most - 1) / most;          // groups of a split
-  per = (per + kWaves - 1) / kWaves * kWaves;
+  if (cache_len <= kSoloEntries || most == 1) return p;
+  const auto splits = [&](int64_t per) { return (groups + per - 1) / per; };
+  int64_t per = split_groups(groups, most);
+  const int64_t even = split_groups(groups, std::clamp<int64_t>(kTargetBlocks / heads, 1, most));   // one round, if it is full
+  if (!ragged && heads * splits(even) > kTargetBlocks * 9 / 10 && heads * splits(even) <= kTargetBlocks &&
+      splits(even) * even - groups <= groups / 16)
+    per = even;
+  if (heads * splits(per) < kTargetBlocks * 3 / 2)
+    while (heads * splits(per) > kTargetBlocks && per < groups) per += kWaves;
   p.chunk = (int)(per * kGroup);
-  p.slots = (int)((groups + per - 1) / per) + 1;
+  p.slots = (int)splits(per) + 1;
   p.bytes = partial_bytes(heads, p.slots, d, G, &p.ml_bytes);
   return p;
 }
@@ -629,8 +665,8 @@ Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G, bool ragged
 size_t decode8_workspace_bound(int64_t heads, int capacity, int d, int G) {
   size_t ml;
   const int64_t groups = ((int64_t)capacity + kGroup - 1) / kGroup;
-  const int64_t most = most_splits(heads, groups, true);
-  return capacity <= kSolo8Entries || most == 1 ? 0 : partial_bytes(heads, most + 1, d, G, &ml);
+  const int64_t most = most_splits(heads, groups);
+  return capacity <= kSoloEntries || most == 1 ? 0 : partial_bytes(heads, most + 1, d, G, &ml);
 }
 
 hipError_t launch_decode8(int64_t heads, int hkv, int d, int G, int dtype, float scale, const Decode8Plan& p,

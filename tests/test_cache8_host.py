@@ -79,8 +79,16 @@ def test_the_capacity_workspace_passes_at_every_length():
         c = cache(block=block, capacity=cap)
         S.lib.selkv_decode8_workspace_size(p, c, ctypes.byref(need))
         for n in range(0, cap, 37):
-            assert attn(p, c, cache_len=n, ws_bytes=need.value) == EHIP
-            assert append(p, c, cache_len=n, ws_bytes=need.value) == EHIP
+            for lens in (NULL, FAKE):
+                assert attn(p, c, cache_len=n, lens=lens, ws_bytes=need.value) == EHIP
+                assert append(p, c, cache_len=n, lens=lens, ws_bytes=need.value) == EHIP
+    for heads in (1, 2, 7, 60, 100, 255, 256, 400, 768, 769, 2304, 2305, 65535):
+        p = S.params(batch=heads, n_heads_kv=1, group=2)
+        c = cache(capacity=1 << 28)
+        assert S.lib.selkv_decode8_workspace_size(p, c, ctypes.byref(need)) == 0
+        for n in (0, 769, 1000, 2048, 5000, 12801, 25600, 102400, 1 << 20, (1 << 28) - 1):
+            for lens in (NULL, FAKE):
+                assert attn(p, c, cache_len=n, lens=lens, ws_bytes=need.value) == EHIP, (heads, n)
 
 
 @no_gpu
