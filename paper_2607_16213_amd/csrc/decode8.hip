@@ -48,7 +48,7 @@ constexpr int kMaxSplit = 512;
 // second kernel, 900 entries 11.8 and 10.4
 constexpr int kSoloEntries = 768;
 constexpr int kCUs = 256;
-constexpr int kFewSlots = 16;
+constexpr int kFewSlots = 8;
 
 struct DecodeArgs8 {
   Cache8 c;
@@ -504,12 +504,13 @@ __global__ __launch_bounds__(ROLE == kSolo8 ? 2 * kThreads : kThreads,
 
 // Combines the partials of the query heads, in slot order.  A unit of d/4 threads takes four channels each of the
 // slots sub, sub + SUB, ... of a query head and loads kBatch of them at a time; with SUB > 1 the runs then meet in
-// LDS, in order.  SUB = 1 where a head has few slots (a unit then has them all in flight at once), otherwise the
-// whole workgroup takes one query head: 100 slots in one trip to memory.
+// LDS, in order.  SUB = 1 where a head has few slots, otherwise the whole workgroup takes one query head: 64 slots in
+// one trip to memory.  The kernel is a chain of latencies (3 - 4 us, two of them what any kernel takes), so its code
+// is kept short.
 template <int D, int SUB>
 __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int qheads) {
   constexpr int kUnits = 256 / (D / 4);   // 8 or 16
-  constexpr int kBatch = D == 128 || SUB == 1 ? 16 : 8;
+  constexpr int kBatch = 8;
   static_assert(SUB == 1 || SUB == kUnits, "a unit is a query head, or all of them are one");
   __shared__ float s_m[kUnits], s_l[kUnits];
   __shared__ __align__(16) float s_o[kUnits][D];
@@ -524,24 +525,19 @@ __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int 
   const float* po = a.part_o + ((size_t)head * a.slots * a.G + g) * D + c4 * 4;
   float m = kNegInf, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < slots; s0 += SUB * kBatch) {
+  for (int s0 = sub; s0 < slots; s0 += SUB * kBatch) {
     f32x4 ov[kBatch];
     float2 v[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (s0 + u * SUB < slots) {
-        const int sl = min(s0 + u * SUB + sub, slots - 1);
-        ov[u] = *reinterpret_cast<const f32x4*>(po + (size_t)sl * a.G * D);
-        v[u] = ml[(size_t)sl * a.G];
-      }
+      const int sl = min(s0 + u * SUB, slots - 1);
+      ov[u] = *reinterpret_cast<const f32x4*>(po + (size_t)sl * a.G * D);
+      v[u] = ml[(size_t)sl * a.G];
     }
     float M = m;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (s0 + u * SUB + sub >= slots) {
-        v[u] = make_float2(kNegInf, 0.f);
-        ov[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
+      if (s0 + u * SUB >= slots) v[u].x = kNegInf;     // the last slot again: weight 0
       M = fmaxf(M, v[u].x);
     }
     const float c = weight_of(m, M);
@@ -549,12 +545,10 @@ __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int 
     o *= c;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (s0 + u * SUB < slots) {
-        const float w = weight_of(v[u].x, M);
-        l = fmaf(v[u].y, w, l);
+      const float w = weight_of(v[u].x, M);
+      l = fmaf(v[u].y, w, l);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(ov[u][e], w, o[e]);
-      }
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(ov[u][e], w, o[e]);
     }
     m = M;
   }
@@ -569,18 +563,17 @@ __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int 
       s_l[unit] = l;
     }
     __syncthreads();
-    for (int dd = threadIdx.x; dd < D; dd += 256) {
-      float M = kNegInf, L = 0.f, t = 0.f;
+    if (threadIdx.x >= D) return;
+    float M = kNegInf, L = 0.f, t = 0.f;
 #pragma unroll
-      for (int k = 0; k < kUnits; ++k) M = fmaxf(M, s_m[k]);
+    for (int k = 0; k < kUnits; ++k) M = fmaxf(M, s_m[k]);
 #pragma unroll
-      for (int k = 0; k < kUnits; ++k) {
-        const float w = weight_of(s_m[k], M);
-        t = fmaf(s_o[k][dd], w, t);
-        L = fmaf(s_l[k], w, L);
-      }
-      a.out[(size_t)qh * D + dd] = L > 0.f ? t / L : 0.f;
+    for (int k = 0; k < kUnits; ++k) {
+      const float w = weight_of(s_m[k], M);
+      t = fmaf(s_o[k][threadIdx.x], w, t);
+      L = fmaf(s_l[k], w, L);
     }
+    a.out[(size_t)qh * D + threadIdx.x] = L > 0.f ? t / L : 0.f;
   }
 }
 

@@ -274,6 +274,77 @@ def test_attn_lowest_bias_and_masked_garbage(S, dtype, code):
     check_attn(m2, run_attn(S, p2, c2, q, bias, n), q, bias, G, d, "garbage")
 
 
+@pytest.mark.parametrize("B,H,G,d,n", [
+    (1, 8, 4, 128, 768), (1, 8, 4, 128, 769),          # one workgroup a head, and splits
+    (1, 1, 2, 64, 20000),                              # more partials than one trip of the combining kernel
+    (1, 2, 8, 128, 9000), (4, 6, 1, 64, 2700),
+    (32, 8, 1, 64, 3000),                              # a round of workgroups that comes out even
+    (33, 8, 2, 64, 300), (96, 8, 3, 64, 1100),         # more heads than CUs: four waves a head, without and with the tail
+])
+def test_attn_work_division(S, B, H, G, d, n):
+    """Both sides of the rules that divide the work, with a step on top."""
+    g = gen(n)
+    p, c, m = make(S, B, H, G, d, "bf16", "int8", 64, n + 1)
+    K, V = U.rows(g, B, H, n, d, dtype="bf16"), U.rows(g, B, H, n, d, dtype="bf16")
+    S.cache8_write(p, c, K, V, 0)
+    some = sorted({0, B // 2, B - 1})                  # sequences that are compared
+    keep = U.Model(len(some), H, d, 64, "int8")
+    for i, b in enumerate(some):
+        keep.append(i, K[b], V[b])
+    q = torch.randn((B, H * G, d), generator=g, device=DEV).to(torch.bfloat16)
+    bias = torch.rand((B, H, c.capacity), generator=g, device=DEV)
+    out = run_attn(S, p, c, q, bias, n)
+    check_attn(keep, out[some], q[some], bias[some], G, d, f"n={n}")
+    assert torch.equal(out, run_attn(S, p, c, q, bias, n))
+    k, v = U.rows(g, B, H, d, dtype="bf16"), U.rows(g, B, H, d, dtype="bf16")
+    dec = S.Decoder8(p, c)
+    out = dec.step(q, k, v, n, bias)
+    for i, b in enumerate(some):
+        kk, vv = keep.values(i)
+        kk, vv = np.concatenate((kk, U.host(k[b])[:, None]), 1), np.concatenate((vv, U.host(v[b])[:, None]), 1)
+        want, big = U.attention(U.host(q[b]), kk, vv, U.host(bias[b, :, :n + 1]), G, U.scale_of(d))
+        U.assert_near(U.host(out[b]), want, big, f"step, sequence {b}")
+
+
+def test_attn_lengths_far_below_the_bound(S):
+    """A bound of the whole capacity and short sequences: their slots are cut from their own lengths."""
+    B, H, G, d, cap = 5, 2, 4, 128, 64 * 400
+    g = gen(55)
+    p, c, m = make(S, B, H, G, d, "bf16", "e4m3", 64, cap)
+    lens = [5, 300, 2000, 0, 9000]
+    K, V = U.rows(g, B, H, 9000, d, dtype="bf16"), U.rows(g, B, H, 9000, d, dtype="bf16")
+    S.cache8_write(p, c, K, V, 0, i32(*([0] * B)), i32(*lens))
+    for b in range(B):
+        m.append(b, K[b, :, :lens[b]], V[b, :, :lens[b]])
+    q = torch.randn((B, H * G, d), generator=g, device=DEV).to(torch.bfloat16)
+    check_attn(m, run_attn(S, p, c, q, None, cap, i32(*lens)), q, None, G, d, "short")
+    uniform = run_attn(S, p, c, q, None, 5)            # the same number for all: only what every sequence holds
+    tail = c.k_tail[0, :, :5]
+    out0, big = U.attention(U.host(q[0]), U.host(tail).astype(np.float64), U.host(c.v_tail[0, :, :5]).astype(np.float64),
+                            None, G, U.scale_of(d))
+    U.assert_near(U.host(uniform[0]), out0, big, "uniform")
+
+
+def test_two_streams_on_one_cache(S):
+    """Two decodes over the same cache at once, each with a workspace of its own, give what one alone gives."""
+    H, G, d, n = 8, 4, 128, 6000
+    g = gen(12)
+    p, c, m = make(S, 1, H, G, d, "bf16", "int8", 64, n)
+    K, V = U.rows(g, 1, H, n, d, dtype="bf16"), U.rows(g, 1, H, n, d, dtype="bf16")
+    S.cache8_write(p, c, K, V, 0)
+    qs = [torch.randn((1, H * G, d), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2)]
+    alone = [run_attn(S, p, c, q, None, n) for q in qs]
+    streams, wss = [torch.cuda.Stream() for _ in range(2)], [S.decode8_workspace(p, c) for _ in range(2)]
+    outs = [torch.zeros_like(alone[0]) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, st, ws, out in zip(qs, streams, wss, outs):
+            S.decode8_attn(p, c, q, None, n, out, ws, stream=st)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, outs):
+        assert torch.equal(a, b)
+
+
 def test_attn_scale_and_long_logits(S):
     """A scale of its own, and logits far apart (one entry takes all the weight)."""
     H, G, d, block, n = 4, 4, 128, 64, 5000
