@@ -402,9 +402,9 @@ SELKV_API selkv_status selkv_decode_append(const selkv_params* p, const void* q,
  * is the number of entries of sequence b and cache_len an upper bound of them
  * that the host knows; the library only reads lens (the caller advances it
  * after a call that appends), so a captured call follows it from replay to
- * replay.  A negative lens[b] marks a sequence that takes no part: nothing of
- * it is stored, and its decode outputs are 0.  A lens[b] above cache_len is
- * taken as cache_len.
+ * replay.  A lens[b] outside [0, cache_len] (-1, say, or a full sequence in a
+ * step whose cache_len is capacity - 1) marks a sequence that takes no part:
+ * nothing of it is stored or read, and its decode outputs are 0.
  * ------------------------------------------------------------------------- */
 
 typedef enum selkv_code8 {
@@ -449,8 +449,9 @@ SELKV_API selkv_status selkv_cache8_write(const selkv_params* p, const selkv_cac
                                           const int32_t* counts, hipStream_t stream);
 
 /* Read entries first .. first + count - 1 of every sequence back as rows in
- * the storage type: code * scale rounded once to kv_dtype, the rows of the
- * open block as they are (what the decode attends over).
+ * the storage type: code * scale rounded to fp32 (to its largest number where
+ * the product passes it) and to kv_dtype, the rows of the open block as they
+ * are.
  * In:  the cache; 0 <= first, count >= 1, first + count <= capacity.
  * Out: K_out, V_out [B, H_kv, count, d] (kv_dtype); rows of entries that a
  *      sequence does not hold are left as they were.

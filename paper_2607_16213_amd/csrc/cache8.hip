@@ -15,6 +15,8 @@
 // bf16 are written in 909 us, 5.5 TB/s, against 926 with ordinary stores and 968
 // with each thread's codes stored as it holds them (16-byte pieces 64 bytes
 // apart); a layer of them is read back in 24.9 us, 6.3 TB/s, against 33.9.
+#include <float.h>
+
 #include "cache8.hpp"
 
 namespace selkv {
@@ -37,13 +39,12 @@ __global__ __launch_bounds__(kThreads) void cache8_write_kernel(WriteArgs a) {
   __shared__ float s_max[4];
   __shared__ __align__(16) char s_codes[kThreads * 64];   // the workgroup's codes, as they lie in the cache
   const bool is_v = blockIdx.z != 0;
-  const int64_t head = blockIdx.y;
-  const int b = (int)(head / a.hkv);
+  const uint32_t head = blockIdx.y;
   const int block = a.c.block, cap = a.c.capacity;
-  const int len = entries_of(a.n, b);
+  const int len = entries_of(a.n, head, a.hkv);
   if (len < 0) return;
   int cnt = a.n_new;
-  if (a.counts) cnt = max(0, min(a.counts[b], cnt));
+  if (a.counts) cnt = max(0, min(a.counts[head / (uint32_t)a.hkv], cnt));
   cnt = min(cnt, cap - len);
   const int r0 = len % block, fb = len / block;   // rows in the tail, first block the call may complete
   const int full = (len + cnt) / block - fb;      // blocks that it completes
@@ -98,8 +99,8 @@ __global__ __launch_bounds__(kThreads) void cache8_read_kernel(ReadArgs a) {
   constexpr int RB = D * (int)sizeof(T);
   constexpr int kTiles = kThreads / (D / 4);   // 16-token tiles of a workgroup
   const bool is_v = blockIdx.z != 0;
-  const int64_t head = blockIdx.y;
-  const int len = entries_of(a.n, (int)(head / a.hkv));
+  const uint32_t head = blockIdx.y;
+  const int len = entries_of(a.n, head, a.hkv);
   const int block = a.c.block, cap = a.c.capacity;
   const int end = min(a.first + a.count, len);
   const int c4 = threadIdx.x % (D / 4);
@@ -135,7 +136,11 @@ __global__ __launch_bounds__(kThreads) void cache8_read_kernel(ReadArgs a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f[i][e] *= sc;
+      for (int e = 0; e < 4; ++e) {
+        f[i][e] *= sc;
+        // 127 * (a / 127) may round past the largest number where a is next to it
+        if constexpr (sizeof(T) == 4) f[i][e] = fminf(fmaxf(f[i][e], -FLT_MAX), FLT_MAX);
+      }
       x[i].set(f[i]);
     }
   } else {

@@ -20,9 +20,12 @@ constexpr float kTinyBlock = 0x1p-100f;   // below it top / a nears the end of f
 template <int CODE>
 __device__ __forceinline__ constexpr float code_top() { return CODE == SELKV_I8 ? 127.f : 448.f; }
 
-// Entries of sequence b: lens[b] where lens is set, at most cache_len; negative: the sequence takes no part.
-__device__ __forceinline__ int entries_of(const Lens8& n, int b) {
-  return n.lens ? min(n.lens[b], n.cache_len) : n.cache_len;
+// Entries of sequence head / hkv: lens[] where lens is set; negative where that is outside [0, cache_len], the sequence
+// then takes no part (appended to at another place it would lose entries).
+__device__ __forceinline__ int entries_of(const Lens8& n, uint32_t head, int hkv) {
+  if (!n.lens) return n.cache_len;
+  const int len = n.lens[head / (uint32_t)hkv];
+  return (uint32_t)len <= (uint32_t)n.cache_len ? len : -1;
 }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));

@@ -394,7 +394,7 @@ __global__ __launch_bounds__(ROLE == kSolo8 ? 2 * kThreads : kThreads,
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
   const int shift = a.block_shift, block = 1 << shift, cap = a.c.capacity;
-  const int len = a.n.lens ? min(a.n.lens[head / (uint32_t)a.hkv], a.n.cache_len) : a.n.cache_len;
+  const int len = entries_of(a.n, head, a.hkv);
   const bool active = len >= 0;
   const int whole = active ? len >> shift << shift : 0;  // entries held as codes
   const int rest = active ? len - whole : 0;             // rows in the tail
@@ -517,7 +517,7 @@ __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int 
   const int c4 = threadIdx.x % (D / 4), unit = threadIdx.x / (D / 4), sub = SUB == 1 ? 0 : unit;
   const uint32_t qh = SUB == 1 ? min(blockIdx.x * kUnits + unit, (uint32_t)qheads - 1) : blockIdx.x;
   const uint32_t head = qh / (uint32_t)a.G, g = qh % (uint32_t)a.G;
-  const int len = a.n.lens ? min(a.n.lens[head / (uint32_t)a.hkv], a.n.cache_len) : a.n.cache_len;
+  const int len = entries_of(a.n, head, a.hkv);
   const int whole = len > 0 ? len >> a.block_shift << a.block_shift : 0;
   const int chunk = chunk_of(a, whole);
   const int slots = 1 + (whole + chunk - 1) / chunk;    // the tail's and those of the splits that had entries

@@ -127,6 +127,43 @@ def test_write_extreme_values(S, dtype, code):
     U.assert_holds(c, m)
     assert np.isfinite(U.host(c.K)).all() and np.isfinite(U.host(c.V)).all()
     assert torch.isfinite(c.k_scale).all() and torch.isfinite(c.v_scale).all()
+    Ko, Vo = torch.empty_like(K), torch.empty_like(V)
+    S.cache8_read(p, c, Ko, Vo, 12 * block)
+    assert torch.isfinite(Ko).all() and torch.isfinite(Vo).all()
+    largest = torch.finfo(dt).max * (1 - 2.0 ** -7)          # within a step of bf16 of where they were
+    assert Ko[0, 0, 8 * block, 0] >= largest and Vo[0, 0, 9 * block, 0] <= -largest
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_a_full_sequence_keeps_its_entries(S, code):
+    """Steps and writes in a graph-like loop whose bound is capacity - 1: a sequence that has become full is left alone."""
+    B, H, G, d, block, cap = 3, 2, 2, 64, 16, 32
+    g = gen(2)
+    p, c, m = make(S, B, H, G, d, "bf16", code, block, cap)
+    K, V = U.rows(g, B, H, cap, d, dtype="bf16"), U.rows(g, B, H, cap, d, dtype="bf16")
+    have = [cap, cap - 1, 20]
+    S.cache8_write(p, c, K, V, cap, i32(0, 0, 0), i32(*have))
+    for b in range(B):
+        m.append(b, K[b, :, :have[b]], V[b, :, :have[b]])
+    lens, bias, dec = i32(*have), torch.ones((B, H, cap), device=DEV), S.Decoder8(p, c)
+    for _ in range(3):
+        now = lens.tolist()
+        k, v = U.rows(g, B, H, d, dtype="bf16"), U.rows(g, B, H, d, dtype="bf16")
+        q = torch.randn((B, H * G, d), generator=g, device=DEV).to(torch.bfloat16)
+        out = dec.step(q, k, v, cap - 1, bias, lens)
+        for b in range(B):
+            if now[b] >= cap:
+                assert (out[b] == 0).all()
+            else:
+                assert (out[b] != 0).any()
+                m.append(b, k[b][:, None], v[b][:, None])
+        U.assert_holds(c, m, str(now))
+        lens += 1
+    assert (bias[0] == 1).all()
+    before = [t.clone() for t in (c.K, c.V, c.k_tail, c.v_tail)]
+    S.cache8_write(p, c, K, V, cap, i32(cap, cap + 1, -1))
+    for t, x in zip((c.K, c.V, c.k_tail, c.v_tail), before):
+        assert torch.equal(t.view(torch.uint8), x.view(torch.uint8))
 
 
 # ---- read ----------------------------------------------------------------------------------------------------------
@@ -231,12 +268,13 @@ def test_attn_ragged_and_masked(S, B, H, G, d, block, cap, dtype, code):
     bias[B // 2] = NEG_INF
     bias[B - 1, :, : lens[B - 1] // 2] = NEG_INF
     check_attn(m, run_attn(S, p, c, q, bias, cap, i32(*lens)), q, bias, G, d, "masked")
-    # a sequence that takes no part, and a length beyond the bound, which is cut to it
+    # lengths outside [0, bound]: the sequence takes no part
     lens2 = list(lens)
     lens2[0], lens2[B - 1] = cap + 5, -1
     out = run_attn(S, p, c, q, None, cap, i32(*lens2))
-    assert (out[B - 1] == 0).all()
-    m.k[B - 1], m.v[B - 1] = m.k[B - 1][:, :0], m.v[B - 1][:, :0]
+    for b in (0, B - 1):
+        assert (out[b] == 0).all()
+        m.k[b], m.v[b] = m.k[b][:, :0], m.v[b][:, :0]
     check_attn(m, out, q, None, G, d, "no part")
 
 
