@@ -448,8 +448,8 @@ class Cache8:
 
 
 def _check_cache8(p, cache, tensors, lens, counts, stream):
-    """Checks the cache against p and the current device, and (tensor, shape, dtype, name) of every tensor.  The launch
-    goes to the current device, so all of them have to be there."""
+    """Checks the cache against p and the current device, and (tensor, shape, dtype, name) of every tensor; returns the
+    stream's handle.  The launch goes to the current device, so all of them have to be there."""
     if cache._of != (p.batch, p.n_heads_kv, p.head_dim, p.kv_dtype):
         raise ValueError(f"the cache was made for (batch, n_heads_kv, head_dim, kv_dtype) = {cache._of}")
     dev = cache.device
@@ -460,9 +460,10 @@ def _check_cache8(p, cache, tensors, lens, counts, stream):
     if counts is not None:
         tensors += ((counts, (p.batch,), _I32, "counts"),)
     for t, shape, dtype, name in tensors:
-        if not _ok(t, shape, dtype) or t.device != dev:
+        if not (t.device == dev and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
             _dev(t, shape, dtype, name)
             raise ValueError(f"{name} is on {t.device}, the cache on {dev}")
+    return _raw_stream(dev.index) if stream is None else stream.cuda_stream
 
 
 def cache8_write(p, cache, K_new, V_new, cache_len, lens=None, counts=None, stream=None):
@@ -472,11 +473,11 @@ def cache8_write(p, cache, K_new, V_new, cache_len, lens=None, counts=None, stre
         raise ValueError("K_new must have four dimensions")
     n_new = K_new.shape[2]
     new, dt = (p.batch, p.n_heads_kv, n_new, p.head_dim), _kvdt(p)
-    _check_cache8(p, cache, ((K_new, new, dt, "K_new"), (V_new, new, dt, "V_new")), lens, counts, stream)
+    on = _check_cache8(p, cache, ((K_new, new, dt, "K_new"), (V_new, new, dt, "V_new")), lens, counts, stream)
     if n_new == 0:
         return
     st = lib.selkv_cache8_write(p, cache.c, K_new.data_ptr(), V_new.data_ptr(), n_new, int(cache_len), _ptr(lens),
-                                _ptr(counts), _stream(stream))
+                                _ptr(counts), on)
     if st:
         raise SelkvError(st, "selkv_cache8_write")
 
@@ -488,11 +489,11 @@ def cache8_read(p, cache, K_out, V_out, cache_len, first=0, lens=None, stream=No
         raise ValueError("K_out must have four dimensions")
     count = K_out.shape[2]
     out, dt = (p.batch, p.n_heads_kv, count, p.head_dim), _kvdt(p)
-    _check_cache8(p, cache, ((K_out, out, dt, "K_out"), (V_out, out, dt, "V_out")), lens, None, stream)
+    on = _check_cache8(p, cache, ((K_out, out, dt, "K_out"), (V_out, out, dt, "V_out")), lens, None, stream)
     if count == 0:
         return
     st = lib.selkv_cache8_read(p, cache.c, K_out.data_ptr(), V_out.data_ptr(), int(first), count, int(cache_len),
-                               _ptr(lens), _stream(stream))
+                               _ptr(lens), on)
     if st:
         raise SelkvError(st, "selkv_cache8_read")
 
@@ -513,11 +514,13 @@ def decode8_attn(p, cache, q, bias_in, cache_len, out, ws, lens=None, stream=Non
     B, H = p.batch, p.n_heads_kv
     qs = (B, H * p.group, p.head_dim)
     ts = ((q, qs, _kvdt(p), "q"), (out, qs, _F32, "out"))
+    if ws is not None and ws.device != cache.device:
+        raise ValueError(f"the workspace is on {ws.device}, the cache on {cache.device}")
     if bias_in is not None:
         ts += ((bias_in, (B, H, cache.capacity), _F32, "bias"),)
-    _check_cache8(p, cache, ts, lens, None, stream)
+    on = _check_cache8(p, cache, ts, lens, None, stream)
     st = lib.selkv_decode8_attn(p, cache.c, q.data_ptr(), _ptr(bias_in), int(cache_len), _ptr(lens), out.data_ptr(),
-                                _ptr(ws), _nbytes(ws), _stream(stream))
+                                _ptr(ws), _nbytes(ws), on)
     if st:
         raise SelkvError(st, "selkv_decode8_attn")
 
@@ -528,11 +531,13 @@ def decode8_append(p, cache, q, k_new, v_new, bias_io, cache_len, out, ws, lens=
     B, H, d = p.batch, p.n_heads_kv, p.head_dim
     dt, qs = _kvdt(p), (B, H * p.group, d)
     ts = ((q, qs, dt, "q"), (k_new, (B, H, d), dt, "k_new"), (v_new, (B, H, d), dt, "v_new"), (out, qs, _F32, "out"))
+    if ws is not None and ws.device != cache.device:
+        raise ValueError(f"the workspace is on {ws.device}, the cache on {cache.device}")
     if bias_io is not None:
         ts += ((bias_io, (B, H, cache.capacity), _F32, "bias"),)
-    _check_cache8(p, cache, ts, lens, None, stream)
+    on = _check_cache8(p, cache, ts, lens, None, stream)
     st = lib.selkv_decode8_append(p, cache.c, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _ptr(bias_io),
-                                  int(cache_len), _ptr(lens), out.data_ptr(), _ptr(ws), _nbytes(ws), _stream(stream))
+                                  int(cache_len), _ptr(lens), out.data_ptr(), _ptr(ws), _nbytes(ws), on)
     if st:
         raise SelkvError(st, "selkv_decode8_append")
 

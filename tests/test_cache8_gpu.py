@@ -616,6 +616,10 @@ def test_refusals_with_device_tensors(S):
         S.cache8_write(p, c, new, new, 60)
     with pytest.raises(ValueError, match="bias"):
         S.decode8_attn(p, c, q, torch.zeros((2, 2, 60), device=DEV), 10, out, ws)
+    with pytest.raises(ValueError, match="workspace"):
+        S.decode8_attn(p, c, q, None, 10, out, ws.cpu())
+    with pytest.raises(ValueError, match="out has"):
+        S.decode8_attn(p, c, q, None, 10, out.half(), ws)
     with pytest.raises(ValueError, match="was made for"):
         S.decode8_attn(S.params(batch=1, n_heads_kv=2, group=2, head_dim=64), c, q, None, 10, out, ws)
     with pytest.raises(S.SelkvError, match="EINVAL"):
