@@ -12,9 +12,12 @@
 // Read: a thread takes 16 tokens x 4 channels, as the write does.
 // Both are bound by the memory they move.  Stores pass the caches' replacement
 // order by (nothing here is read again): 32 layers x 8 heads x 25600 rows of
-// bf16 are written in 909 us, 5.5 TB/s, against 926 with ordinary stores and 968
-// with each thread's codes stored as it holds them (16-byte pieces 64 bytes
-// apart); a layer of them is read back in 24.9 us, 6.3 TB/s, against 33.9.
+// bf16 are written in 890 us, 5.7 TB/s, against 914 with ordinary stores (and
+// 4% more where each thread stores its codes as it holds them, 16-byte pieces
+// 64 bytes apart); a layer of them is read back in 24.9 us, 6.3 TB/s, against
+// 33.9.  A finite block's codes need no clamp and few instructions a value
+// (cache8.hpp), which short calls feel: 8191 rows of a layer take 10.1 us, 11.4
+// with clamps and conversions one by one.
 #include <float.h>
 
 #include "cache8.hpp"

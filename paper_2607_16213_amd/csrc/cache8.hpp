@@ -28,6 +28,7 @@ __device__ __forceinline__ int entries_of(const Lens8& n, uint32_t head, int hkv
   return (uint32_t)len <= (uint32_t)n.cache_len ? len : -1;
 }
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -43,6 +44,12 @@ template <> struct Quad<float> {
   __device__ __forceinline__ float get(int e) const {
     return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w);
   }
+  // Largest magnitude so far as its bits (they order as the numbers do); bits(m): those of an fp32 number.
+  __device__ __forceinline__ uint32_t largest(uint32_t m) const {
+    const uint32_t k = 0x7fffffffu;
+    return max(max(max(m, w.x & k), max(w.y & k, w.z & k)), w.w & k);
+  }
+  __device__ static __forceinline__ uint32_t bits(uint32_t m) { return m; }
   __device__ __forceinline__ void set(const float (&x)[4]) {
     w = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
   }
@@ -57,6 +64,12 @@ template <> struct Quad<bf16_t> {
     const uint32_t x = e < 2 ? w.x : w.y;
     return __uint_as_float((e & 1) ? (x & 0xffff0000u) : (x << 16));
   }
+  __device__ __forceinline__ uint32_t largest(uint32_t m) const {   // of the even and of the odd elements
+    const uint32_t k = 0x7fff7fffu;
+    const u16x2 r = __builtin_elementwise_max(__builtin_bit_cast(u16x2, w.x & k), __builtin_bit_cast(u16x2, w.y & k));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), r));
+  }
+  __device__ static __forceinline__ uint32_t bits(uint32_t m) { return max(m << 16, m & 0xffff0000u); }
   __device__ __forceinline__ void set(const float (&x)[4]) {
     w.x = f32_to_bf16(x[0]) | ((uint32_t)f32_to_bf16(x[1]) << 16);
     w.y = f32_to_bf16(x[2]) | ((uint32_t)f32_to_bf16(x[3]) << 16);
@@ -73,26 +86,27 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a < __builtin_huge_valf() ? a : 0.f;
 }
 
-// Codes of four values, in the bytes of one word.  fminf / fmaxf drop a NaN, so it is set to 0 first.
+// Codes of four finite values of a block whose inv is top / a, in the bytes of one word: none is larger than a, so the
+// products need no clamp (127 or 448 and an ulp round to the largest code).  int8: adding 1.5 * 2^23 rounds to the
+// nearest integer, ties to even, and leaves it in the low byte; the product is rounded on its own, never fused.
 template <int CODE>
 __device__ __forceinline__ uint32_t encode4(float x0, float x1, float x2, float x3, float inv) {
-  float y[4] = {x0 * inv, x1 * inv, x2 * inv, x3 * inv};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[i] = y[i] == y[i] ? y[i] : 0.f;
-    y[i] = fminf(fmaxf(y[i], -code_top<CODE>()), code_top<CODE>());
-  }
+#pragma clang fp contract(off)
   if constexpr (CODE == SELKV_I8) {
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int)rintf(y[i]) & 0xffu) << (8 * i);
-    return w;
+    constexpr float kRound = 12582912.f;
+    const uint32_t y0 = __float_as_uint(x0 * inv + kRound), y1 = __float_as_uint(x1 * inv + kRound);
+    const uint32_t y2 = __float_as_uint(x2 * inv + kRound), y3 = __float_as_uint(x3 * inv + kRound);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(y3, y2, 0x0c0c0400u), __builtin_amdgcn_perm(y1, y0, 0x0c0c0400u),
+                                 0x05040100u);
   } else {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x0 * inv, x1 * inv, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(x2 * inv, x3 * inv, w, true);
     return (uint32_t)w;
   }
 }
+
+// A value that may be infinite or NaN, brought into [-a, a]: NaN to 0.
+__device__ __forceinline__ float tame(float x, float a) { return x == x ? fminf(fmaxf(x, -a), a) : 0.f; }
 
 // The value (without the scale) of byte B of a word of codes.
 template <int CODE, int B>
@@ -133,13 +147,22 @@ __device__ __forceinline__ void quantise_blocks(bool on, const BlockThread& bt, 
                                                 char* codes, float* scale, float (&s_max)[4]) {
   Quad<T> x[16];
   float a = 0.f;
+  bool wild = false;   // the thread holds an infinity or a NaN
   if (on) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i].load(row(i));
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < 16; ++i) m = x[i].largest(m);
+    a = __uint_as_float(Quad<T>::bits(m));
+    wild = Quad<T>::bits(m) >= 0x7f800000u;
+    if (wild) {
+      a = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) a = fmaxf(a, finite_abs(x[i].get(e)));
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a = fmaxf(a, finite_abs(x[i].get(e)));
+    }
   }
   const int per = block / 16 * (D / 4);   // a power of two, 16 .. 256
 #pragma unroll
@@ -157,6 +180,13 @@ __device__ __forceinline__ void quantise_blocks(bool on, const BlockThread& bt, 
   const bool tiny = a < kTinyBlock;
   const float inv = tiny ? 0.f : code_top<CODE>() / a;
   if (bt.tile == 0 && bt.c4 == 0) *scale = tiny ? 0.f : a / code_top<CODE>();
+  if (wild) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float y[4] = {tame(x[i].get(0), a), tame(x[i].get(1), a), tame(x[i].get(2), a), tame(x[i].get(3), a)};
+      x[i].set(y);     // a is an element, so nothing is rounded
+    }
+  }
   if (!is_v) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
