@@ -44,8 +44,8 @@ constexpr int kGroup = 64;            // entries of a wave's step; splits are wh
 constexpr int kTargetBlocks = 768;    // a round of workgroups: three to a CU, what its registers hold
 constexpr int kRounds = 3;
 constexpr int kMaxSplit = 512;
-// up to them a workgroup takes a head by itself: at 8 heads 700 entries take 9.9 us so and 10.4 in splits with the
-// second kernel, 900 entries 11.8 and 10.4
+// up to them a workgroup takes a head by itself: 700 entries of 8 heads take 9.5 us so and 9.9 in splits with the second
+// kernel, 900 entries 11.3 and 10.1
 constexpr int kSoloEntries = 768;
 constexpr int kCUs = 256;
 constexpr int kFewSlots = 8;
@@ -452,22 +452,29 @@ __global__ __launch_bounds__(ROLE == kSolo8 ? 2 * kThreads : kThreads,
                       &s_m[at][g0], &s_l[at][g0], &s_o[at][g0]);
   }
   __syncthreads();
-  for (int idx = threadIdx.x; idx < G * D; idx += NT) {
-    const int g = idx / D, dd = idx % D;
-    float M = kNegInf, l = 0.f, o = 0.f;
+  for (int idx = threadIdx.x; idx < G * (D / 4); idx += NT) {
+    const int g = idx / (D / 4), c4 = idx % (D / 4);
+    float M = kNegInf, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kParts; ++w) M = fmaxf(M, s_m[w][g]);
 #pragma unroll
     for (int w = 0; w < kParts; ++w) {
       const float c = weight_of(s_m[w][g], M);
+      const f32x4 ow = *reinterpret_cast<const f32x4*>(&s_o[w][g][c4 * 4]);
       l = c > 0.f ? fmaf(s_l[w][g], c, l) : l;       // a part without entries may hold anything
-      o = c > 0.f ? fmaf(s_o[w][g][dd], c, o) : o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = c > 0.f ? fmaf(ow[e], c, o[e]) : o[e];
     }
     if (SOLO) {
-      a.out[(size_t)head * G * D + idx] = l > 0.f ? o / l : 0.f;
+      f32x4 r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = l > 0.f ? o[e] / l : 0.f;
+      *reinterpret_cast<f32x4*>(a.out + ((size_t)head * G + g) * D + c4 * 4) = r;
     } else {
-      a.part_o[((size_t)head * a.slots + slot) * G * D + idx] = o;
-      if (dd == 0) a.part_ml[((size_t)head * a.slots + slot) * G + g] = make_float2(M, l);
+      const size_t part = ((size_t)head * a.slots + slot) * G + g;
+      *reinterpret_cast<f32x4*>(a.part_o + part * D + c4 * 4) = o;
+      if (c4 == 0) a.part_ml[part] = make_float2(M, l);
     }
   }
 
@@ -587,8 +594,8 @@ void launch_role(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
 template <typename T, int D, int CODE>
 hipError_t launch_tdc(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
   if (a.slots == 1) {
-    // eight waves where every head has a CU to itself: with more of them four idle ones cost too much (64 x 8 heads
-    // of 300 entries: 15.2 us in four waves each, 17.2 in eight; 32 x 8 heads: 10.9 and 9.3)
+    // eight waves where every head has a CU to itself (32 x 8 heads of 300 entries: 9.2 us, 10.1 in four); with more
+    // heads the four that only see the tail cost too much (64 x 8 heads: 16.6 us, 14.2 in four)
     if (heads <= kCUs) launch_role<T, D, CODE, kSolo8>(heads, a, st);
     else launch_role<T, D, CODE, kSolo4>(heads, a, st);
     return hipGetLastError();
@@ -629,11 +636,11 @@ size_t partial_bytes(int64_t heads, int64_t slots, int d, int G, size_t* ml) {
 }  // namespace
 
 // Splits.  Three rounds of workgroups let fast ones make up for slow ones and for sequences of other lengths: 4 x 32
-// heads of 4096 entries take 29.6 us in 2048 workgroups, 32.3 in 768 (and 35.8 in 512); a ragged batch of 16 x 8 heads
-// of 0 - 8100 entries 34.7 us, 44.1 in 768.  (A sequence of its own length is cut anew on the device, chunk_of.)
-// Every workgroup costs its prologue and its partials, though, so one round is taken where it comes out even: 32 x 8
-// heads of 25641 entries take 299 us in 768 workgroups, 312 in 2304; and a round that is barely exceeded is not begun:
-// 8 heads of 25600 entries take 16.2 us in 400 workgroups, 17.1 in 800.
+// heads of 4096 entries take 30.0 us in 2048 workgroups, 32.8 in 768; a ragged batch of 16 x 8 heads of 0 - 8100
+// entries 34.2 us, 38.7 in one round.  (A sequence of its own length is cut anew on the device, chunk_of.)  Every
+// workgroup costs its prologue and its partials, though, so one round is taken where it comes out even: 32 x 8 heads of
+// 25641 entries take 300 us in 768 workgroups, 310 in 2304; and a round that is barely exceeded is not begun: 8 heads
+// of 25600 entries take 15.3 us in 400 workgroups, 16.6 in 800.
 Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G, bool ragged) {
   Decode8Plan p{};
   const int64_t groups = ((int64_t)cache_len + kGroup - 1) / kGroup;
