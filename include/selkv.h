@@ -439,8 +439,8 @@ SELKV_API void selkv_cache8_init(selkv_cache8* c);
  * on the device) of them, the rows behind being padding that is not read.
  * counts[b] is clamped to [0, n_new] and to the room that is left.
  * In:  K_new, V_new [B, H_kv, n_new, d] (kv_dtype; must not overlap the
- *      cache); 0 <= cache_len, cache_len + n_new <= capacity where counts and
- *      lens are NULL (otherwise cache_len <= capacity).
+ *      cache); 1 <= n_new <= capacity, 0 <= cache_len <= capacity, and
+ *      cache_len + n_new <= capacity where counts and lens are NULL.
  * In/out: the cache.  Entries in front of lens[b] and buffers behind the new
  *      entries keep their contents.
  * Workspace: none. */
@@ -470,7 +470,8 @@ SELKV_API selkv_status selkv_decode8_workspace_size(const selkv_params* p, const
  * out[b, h] = sum_e softmax_e(scale * q[b, h] . K[b, h/G, e] + bias[b, h/G, e]) V[b, h/G, e]
  * over the entries e < lens[b].  bias may be NULL (bitwise the result of a
  * zero bias); a bias of -inf masks its entry whatever the entry holds.  A
- * sequence with no entries, or none that is not masked, gives out = 0.
+ * sequence with no entries, or none that is not masked, gives out = 0; a NaN
+ * in a query, a bias or an unmasked row of the tail reaches the outputs.
  * Queries are not quantised and all sums are fp32.
  * In:  q [B, H_kv*G, d] (kv_dtype); bias [B, H_kv, capacity] fp32 or NULL;
  *      0 <= cache_len <= capacity.  Uses params batch, n_heads_kv, group

@@ -363,6 +363,39 @@ def test_attn_lengths_far_below_the_bound(S):
     U.assert_near(U.host(uniform[0]), out0, big, "uniform")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [20, 300, 3000])
+def test_attn_nan_reaches_the_outputs(S, n, dtype):
+    """A NaN that counts is not lost: of a query its head's outputs, of a tail key all outputs, of a tail value its
+    channel.  (Where nothing counts the outputs are 0.)"""
+    H, G, d, block = 2, 3, 128, 64
+    g = gen(n)
+    p, c, m = make(S, 1, H, G, d, dtype, "int8", block, n)
+    K, V = U.rows(g, 1, H, n, d, dtype=dtype), U.rows(g, 1, H, n, d, dtype=dtype)
+    S.cache8_write(p, c, K, V, 0)
+    q = torch.randn((1, H * G, d), generator=g, device=DEV).to(U.dtype_of(dtype))
+    good = run_attn(S, p, c, q, None, n)
+    q[0, 1, 5] = float("nan")
+    out = run_attn(S, p, c, q, None, n)
+    assert torch.isnan(out[0, 1]).all()
+    keep = [0, 2, 3, 4, 5]
+    assert torch.equal(out[0, keep], good[0, keep])
+    q[0, 1, 5] = 1.0
+    good = run_attn(S, p, c, q, None, n)
+    c.v_tail[0, 0, n % block - 1, 7] = float("nan")
+    out = run_attn(S, p, c, q, None, n)
+    assert torch.isnan(out[0, :G, 7]).all() and torch.isnan(out).sum() == G
+    assert torch.equal(out[0, G:], good[0, G:])
+    c.k_tail[0, 1, n % block - 1, 0] = float("nan")
+    out = run_attn(S, p, c, q, None, n)
+    assert torch.isnan(out[0, G:]).all() and not torch.isnan(out[0, :G, 8:]).any()
+    bias = torch.full((1, H, c.capacity), NEG_INF, device=DEV)
+    assert (run_attn(S, p, c, q, bias, n) == 0).all()
+    bias[0, 1, 3] = float("nan")
+    out = run_attn(S, p, c, q, bias, n)
+    assert (out[0, :G] == 0).all() and torch.isnan(out[0, G:]).all()
+
+
 def test_two_streams_on_one_cache(S):
     """Two decodes over the same cache at once, each with a workspace of its own, give what one alone gives."""
     H, G, d, n = 8, 4, 128, 6000
