@@ -51,9 +51,6 @@ constexpr int kGroup = 64;            // entries of a wave's step; splits are wh
 constexpr int kTargetBlocks = 768;    // a round of workgroups: three to a CU, what its registers hold
 constexpr int kRounds = 3;
 constexpr int kMaxSplit = 512;
-// up to them a workgroup takes a head by itself: 700 entries of 8 heads take 9.5 us so and 9.9 in splits with the second
-// kernel, 900 entries 11.3 and 10.1
-constexpr int kSoloEntries = 768;
 constexpr int kCUs = 256;
 constexpr int kFewSlots = 8;
 
@@ -628,6 +625,11 @@ hipError_t launch_td(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
   return a.c.code == SELKV_I8 ? launch_tdc<T, D, SELKV_I8>(heads, a, st) : launch_tdc<T, D, SELKV_E4M3>(heads, a, st);
 }
 
+// Entries up to which a workgroup takes a head by itself: a call over 500 entries of 8 heads (d = 128) takes 8.4 us so
+// and 10.1 in splits with the second kernel, 700 entries 9.5 and 9.9, 900 entries 11.3 and 10.1; at d = 64, half the
+// work, 900 entries (fp32 queries) 9.3 and 10.3 us, 1500 entries 11.8 and 10.3.
+int solo_entries(int d) { return d == 64 ? 1024 : 768; }
+
 // Most splits of one head: those that give the chip kRounds rounds of workgroups, none shorter than one step of its
 // four waves; none where the heads alone are a round.
 int64_t most_splits(int64_t heads, int64_t groups) {
@@ -659,7 +661,7 @@ Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G, bool ragged
   const int64_t groups = ((int64_t)cache_len + kGroup - 1) / kGroup;
   const int64_t most = most_splits(heads, groups);
   p.slots = 1;
-  if (cache_len <= kSoloEntries || most == 1) return p;
+  if (cache_len <= solo_entries(d) || most == 1) return p;
   const auto splits = [&](int64_t per) { return (groups + per - 1) / per; };
   int64_t per = split_groups(groups, most);
   const int64_t even = split_groups(groups, std::clamp<int64_t>(kTargetBlocks / heads, 1, most));   // one round, if it is full
@@ -679,7 +681,7 @@ size_t decode8_workspace_bound(int64_t heads, int capacity, int d, int G) {
   size_t ml;
   const int64_t groups = ((int64_t)capacity + kGroup - 1) / kGroup;
   const int64_t most = most_splits(heads, groups);
-  return capacity <= kSoloEntries || most == 1 ? 0 : partial_bytes(heads, most + 1, d, G, &ml);
+  return capacity <= solo_entries(d) || most == 1 ? 0 : partial_bytes(heads, most + 1, d, G, &ml);
 }
 
 hipError_t launch_decode8(int64_t heads, int hkv, int d, int G, int dtype, float scale, const Decode8Plan& p,

@@ -313,7 +313,7 @@ def test_attn_lowest_bias_and_masked_garbage(S, dtype, code):
 
 
 @pytest.mark.parametrize("B,H,G,d,n", [
-    (1, 8, 4, 128, 768), (1, 8, 4, 128, 769),          # one workgroup a head, and splits
+    (1, 8, 4, 128, 768), (1, 8, 4, 128, 769), (1, 4, 2, 64, 1024), (1, 4, 2, 64, 1025),   # one workgroup a head, and splits
     (1, 1, 2, 64, 20000),                              # more partials than one trip of the combining kernel
     (1, 2, 8, 128, 9000), (4, 6, 1, 64, 2700),
     (32, 8, 1, 64, 3000),                              # a round of workgroups that comes out even
