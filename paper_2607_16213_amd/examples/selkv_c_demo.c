@@ -14,7 +14,9 @@
  *        V_out [B,H,m,d], bias [B,H,m], out [B,H*G,d], attn [B,H,n],
  *        score [B,H,n-m_r']
  * It then runs the fused selkv_merge_bias into fresh buffers and checks that
- * it reproduces the separate merge and bias bit for bit.
+ * it reproduces the separate merge and bias bit for bit, and keeps the
+ * compressed cache in 8 bits: the decode over the codes must equal the decode
+ * over the rows that selkv_cache8_read gives back, up to fp32 rounding.
  * Exits 0 on success; on failure prints the failing call and its status. */
 #include <stdio.h>
 #include <stdlib.h>
@@ -61,6 +63,53 @@ static void to_file(FILE* f, const void* dev, size_t bytes) {
   HIP_OK(hipMemcpy(h, dev, bytes, hipMemcpyDeviceToHost));
   fwrite(h, 1, bytes, f);
   free(h);
+}
+
+/* The compressed cache as int8 codes: written, read back, decoded over.  Returns the relative 2-norm, squared, between the
+ * decode over the codes and the decode over the rows read back (ws serves the latter), or exits. */
+static double cache8_check(const selkv_params* p, const void* K_out, const void* V_out, const float* bias, size_t m,
+                           const void* q, void* ws, size_t ws_bytes, hipStream_t st) {
+  const size_t heads = (size_t)p->batch * p->n_heads_kv, d = (size_t)p->head_dim, nq = heads * p->group * d;
+  selkv_cache8 c;
+  selkv_cache8_init(&c);
+  const size_t T = (size_t)c.block, cap = (m + T - 1) / T * T;
+  c.capacity = (int32_t)cap;
+  c.K = dev_alloc(heads * cap * d);
+  c.V = dev_alloc(heads * cap * d);
+  c.k_scale = (float*)dev_alloc(heads * (cap / T) * sizeof(float));
+  c.v_scale = (float*)dev_alloc(heads * (cap / T) * sizeof(float));
+  c.k_tail = dev_alloc(heads * T * d * sizeof(float));
+  c.v_tail = dev_alloc(heads * T * d * sizeof(float));
+  void* K8 = dev_alloc(heads * m * d * sizeof(float));
+  void* V8 = dev_alloc(heads * m * d * sizeof(float));
+  float* bias8 = (float*)dev_alloc(heads * cap * sizeof(float));   /* rows of capacity entries */
+  float* out[2] = {(float*)dev_alloc(nq * sizeof(float)), (float*)dev_alloc(nq * sizeof(float))};
+  size_t need = 0;
+  SELKV_OK_(selkv_decode8_workspace_size(p, &c, &need));
+  void* ws8 = dev_alloc(need);
+  SELKV_OK_(selkv_cache8_write(p, &c, K_out, V_out, (int32_t)m, 0, NULL, NULL, st));
+  SELKV_OK_(selkv_cache8_read(p, &c, K8, V8, 0, (int32_t)m, (int32_t)m, NULL, st));
+  HIP_OK(hipMemcpy2DAsync(bias8, cap * sizeof(float), bias, m * sizeof(float), m * sizeof(float), heads,
+                          hipMemcpyDeviceToDevice, st));
+  SELKV_OK_(selkv_decode8_attn(p, &c, q, bias8, (int32_t)m, NULL, out[0], ws8, need, st));
+  SELKV_OK_(selkv_decode_attn(p, q, K8, V8, bias, (int32_t)m, out[1], ws, ws_bytes, st));
+  HIP_OK(hipStreamSynchronize(st));
+  float* h[2];
+  for (int i = 0; i < 2; ++i) {
+    h[i] = (float*)malloc(nq * sizeof(float));
+    if (!h[i]) exit(5);
+    HIP_OK(hipMemcpy(h[i], out[i], nq * sizeof(float), hipMemcpyDeviceToHost));
+  }
+  double off = 0, norm = 0;
+  for (size_t i = 0; i < nq; ++i) {
+    off += ((double)h[0][i] - h[1][i]) * ((double)h[0][i] - h[1][i]);
+    norm += (double)h[1][i] * h[1][i];
+  }
+  void* bufs[] = {c.K, c.V, c.k_scale, c.v_scale, c.k_tail, c.v_tail, K8, V8, bias8, out[0], out[1], ws8};
+  for (size_t i = 0; i < sizeof(bufs) / sizeof(bufs[0]); ++i) HIP_OK(hipFree(bufs[i]));
+  free(h[0]);
+  free(h[1]);
+  return off / norm;
 }
 
 int main(int argc, char** argv) {
@@ -163,6 +212,13 @@ int main(int argc, char** argv) {
     }
     free(ha);
     free(hb);
+  }
+
+  /* both sum the same products in fp32, in another order: a few dozen steps of 2^-24 */
+  const double off8 = cache8_check(&p, K_out, V_out, bias, m, q, ws, ws_bytes, st);
+  if (!(off8 < 1e-5 * 1e-5)) {
+    fprintf(stderr, "the decode over 8-bit codes is %g (squared) off the decode over their values\n", off8);
+    return 8;
   }
 
   FILE* o = fopen(argv[2], "wb");
