@@ -49,7 +49,7 @@ constexpr int kMaxG = 8;
 constexpr int kTailG = 4;             // query heads of a pass over the tail: registers, shared with the codes' loop
 constexpr int kGroup = 64;            // entries of a wave's step; splits are whole multiples of them
 constexpr int kTargetBlocks = 768;    // a round of workgroups: three to a CU, what its registers hold
-constexpr int kRounds = 3;
+constexpr int kRounds = 4;
 constexpr int kMaxSplit = 512;
 constexpr int kCUs = 256;
 constexpr int kFewSlots = 8;
@@ -650,12 +650,12 @@ size_t partial_bytes(int64_t heads, int64_t slots, int d, int G, size_t* ml) {
 
 }  // namespace
 
-// Splits.  Three rounds of workgroups let fast ones make up for slow ones and for sequences of other lengths: 4 x 32
-// heads of 4096 entries take 30.0 us in 2048 workgroups, 32.8 in 768; a ragged batch of 16 x 8 heads of 0 - 8100
-// entries 34.2 us, 38.7 in one round.  (A sequence of its own length is cut anew on the device, chunk_of.)  Every
-// workgroup costs its prologue and its partials, though, so one round is taken where it comes out even: 32 x 8 heads of
-// 25641 entries take 300 us in 768 workgroups, 310 in 2304; and a round that is barely exceeded is not begun: 8 heads
-// of 25600 entries take 15.3 us in 400 workgroups, 16.6 in 800.
+// Splits.  Several rounds of workgroups let fast ones make up for slow ones and for sequences of other lengths: 4 x 32
+// heads of 4096 entries take 29.4 us in 2048 workgroups, 32.8 in 768; ragged batches of up to 8100 entries, 16 x 8 heads
+// 33.9 us, 38.7 in one round and 36.4 in two, 24 x 8 heads 49 us, 53 in two and 52 in three.  (A sequence of its own
+// length is cut anew on the device, chunk_of.)  Every workgroup costs its prologue and its partials, though, so one
+// round is taken where it comes out even: 32 x 8 heads of 25641 entries take 300 us in 768 workgroups, 310 in 2304; and
+// a round that is barely exceeded is not begun: 8 heads of 25600 entries take 15.3 us in 400 workgroups, 16.6 in 800.
 Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G, bool ragged) {
   Decode8Plan p{};
   const int64_t groups = ((int64_t)cache_len + kGroup - 1) / kGroup;
