@@ -344,6 +344,66 @@ def test_attn_work_division(S, B, H, G, d, n):
         U.assert_near(U.host(out[b]), want, big, f"step, sequence {b}")
 
 
+def test_most_heads(S):
+    """65535 KV heads, the most of one call: write, read, decode and a step that completes every block."""
+    B, H, G, d, block, n = 21845, 3, 2, 64, 16, 31
+    g = gen(6)
+    p, c, _ = make(S, B, H, G, d, "bf16", "int8", block, 32)
+    K, V = U.rows(g, B, H, n, d, dtype="bf16"), U.rows(g, B, H, n, d, dtype="bf16")
+    S.cache8_write(p, c, K, V, 0)
+    some = [0, 10000, B - 1]
+    m = U.Model(len(some), H, d, block, "int8")
+    for i, b in enumerate(some):
+        m.append(i, K[b], V[b])
+    q = torch.randn((B, H * G, d), generator=g, device=DEV).to(torch.bfloat16)
+    check_attn(m, run_attn(S, p, c, q, None, n)[some], q[some], None, G, d, "most heads")
+    k, v = U.rows(g, B, H, d, dtype="bf16"), U.rows(g, B, H, d, dtype="bf16")
+    S.Decoder8(p, c).step(q, k, v, n)
+    Ko, Vo = (torch.empty((B, H, 32, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    S.cache8_read(p, c, Ko, Vo, 32)
+    for i, b in enumerate(some):
+        m.append(i, k[b][:, None], v[b][:, None])
+        for got, want in zip((Ko[b], Vo[b]), m.values(i)):
+            assert torch.equal(got.cpu(), torch.from_numpy(want).float().to(torch.bfloat16)), b
+
+
+def test_write_and_read_in_a_replayed_graph(S):
+    """A chunk appended and read back in a captured graph, lengths and counts on the device and changed between replays."""
+    B, H, d, block, cap, n = 3, 2, 128, 32, 320, 40
+    g = gen(14)
+    p, c, m = make(S, B, H, 1, d, "fp32", "e4m3", block, cap)
+    K, V = (torch.zeros((B, H, n, d), device=DEV) for _ in range(2))
+    Ko, Vo = (torch.zeros((B, H, cap, d), device=DEV) for _ in range(2))
+    lens, counts = i32(0, 0, 0), i32(0, 0, 0)
+
+    def chunk():
+        S.cache8_write(p, c, K, V, cap, lens, counts)
+        lens.add_(counts)
+        S.cache8_read(p, c, Ko, Vo, cap, 0, lens)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chunk()                                    # nothing: the counts are 0
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chunk()
+    for i in range(7):
+        K.copy_(U.rows(g, B, H, n, d, dtype="fp32"))
+        V.copy_(U.rows(g, B, H, n, d, dtype="fp32"))
+        take = [n, (i * 17) % (n + 1), i % 2]
+        counts.copy_(i32(*take))
+        chunk() if i == 3 else graph.replay()
+        torch.cuda.synchronize()
+        for b in range(B):
+            m.append(b, K[b, :, :take[b]], V[b, :, :take[b]])
+        U.assert_holds(c, m, f"replay {i}")
+        for b in range(B):
+            for got, want in zip((Ko, Vo), m.values(b)):
+                assert torch.equal(got[b, :, :want.shape[1]].cpu(), torch.from_numpy(want).float()), (i, b)
+
+
 def test_attn_lengths_far_below_the_bound(S):
     """A bound of the whole capacity and short sequences: their slots are cut from their own lengths."""
     B, H, G, d, cap = 5, 2, 4, 128, 64 * 400
