@@ -344,6 +344,40 @@ def test_attn_work_division(S, B, H, G, d, n):
         U.assert_near(U.host(out[b]), want, big, f"step, sequence {b}")
 
 
+def test_odd_alignment_counts_alone_and_short_reads(S):
+    """Biases and scales aligned to an element only, counts without lengths, and a read past what is there."""
+    B, H, G, d, block, cap, dtype = 2, 3, 5, 128, 16, 80 * 16, "bf16"
+    g = gen(41)
+    p, c0, m = make(S, B, H, G, d, dtype, "int8", block, cap)
+    off = lambda shape: torch.full((int(np.prod(shape)) + 1,), float("nan"), device=DEV)[1:].view(shape)
+    c = S.Cache8.over(p, c0.K, c0.V, off(c0.k_scale.shape), off(c0.v_scale.shape), c0.k_tail, c0.v_tail)
+    assert c.k_scale.data_ptr() % 16 == 4
+    first = U.rows(g, B, H, 7, d, dtype=dtype), U.rows(g, B, H, 7, d, dtype=dtype)
+    S.cache8_write(p, c, *first, 0)
+    n = 1000
+    K, V = U.rows(g, B, H, n, d, dtype=dtype), U.rows(g, B, H, n, d, dtype=dtype)
+    counts = [n, 333]
+    S.cache8_write(p, c, K, V, 7, counts=i32(*counts))
+    for b in range(B):
+        m.append(b, first[0][b], first[1][b])
+        m.append(b, K[b, :, :counts[b]], V[b, :, :counts[b]])
+    U.assert_holds(c, m)
+    q = torch.randn((B, H * G, d), generator=g, device=DEV).to(torch.bfloat16)
+    bias = off((B, H, cap)).copy_(torch.randn((B, H, cap), generator=g, device=DEV))
+    check_attn(m, run_attn(S, p, c, q, bias, cap, i32(7 + counts[0], 7 + counts[1])), q, bias, G, d, "odd")
+    few = run_attn(S, p, c, q, bias, 7 + counts[1])          # the entries that both sequences hold
+    m1 = U.Model(1, H, d, block, "int8")
+    m1.append(0, first[0][1], first[1][1])
+    m1.append(0, K[1, :, :counts[1]], V[1, :, :counts[1]])
+    check_attn(m1, few[1:], q[1:], bias[1:], G, d, "few")
+    Ko = torch.full((B, H, 50, d), 2.5, dtype=torch.bfloat16, device=DEV)
+    Vo = torch.full_like(Ko, 2.5)
+    S.cache8_read(p, c, Ko, Vo, 21, 3)
+    for got, want in zip((Ko, Vo), m.values(0)):
+        assert torch.equal(got[0, :, :13].cpu(), torch.from_numpy(want[:, 3:16]).float().to(torch.bfloat16))
+        assert (got[:, :, 18:] == 2.5).all() and (got[:, :, :18] != 2.5).any()
+
+
 def test_most_heads(S):
     """65535 KV heads, the most of one call: write, read, decode and a step that completes every block."""
     B, H, G, d, block, n = 21845, 3, 2, 64, 16, 31
