@@ -27,8 +27,9 @@
 // products: K's multiplies the logits, V's the weights.
 // The running maximum and sum of the softmax, and all accumulators, are fp32.
 // The tail (and the appended token) are few rows, taken in fp32 by lane groups
-// of 16 lanes, each lane d/16 channels.  A masked row (bias -inf) is left out by
-// selection and may hold anything; codes are always finite.
+// of 16 lanes, each lane d/16 channels.  A masked entry (bias -inf) is left out by
+// selection: of the codes its logit, which a NaN or infinite query would spoil,
+// of the tail its rows too, which may hold anything.
 //
 // Bound by HBM where there is work enough: 32 x 8 heads of 25641 entries take
 // 300 us, 5.7 TB/s, the matrix cores busy 11% of the cycles and the VALU 38%
@@ -239,8 +240,8 @@ __device__ __forceinline__ void attend_codes(Wave8<D>& st, const Codes8<D>& x, c
   for (int i = 0; i < 8; ++i) {
     float dot = low ? s[2 + i / 4][i % 4] : s[i / 4][i % 4];
     if constexpr (sizeof(T) == 4) dot += row_ror<8>(low ? s[i / 4][i % 4] : s[2 + i / 4][i % 4]);   // the query's parts
-    y[i] = fmaf(dot, c, has_bias ? x.bias[i / 4][i % 4] : 0.f);
-    y[i] = in ? y[i] : kNegInf;
+    const float b = has_bias ? x.bias[i / 4][i % 4] : 0.f;
+    y[i] = in && b != kNegInf ? fmaf(dot, c, b) : kNegInf;   // selected: the product may be infinite or NaN
     mx = fmaxf(mx, y[i]);
   }
   mx = fmaxf(mx, row_ror<8>(mx));
