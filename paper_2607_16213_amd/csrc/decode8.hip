@@ -11,7 +11,8 @@
 // one more workgroup per head the tail (slot 0, so that it starts first); each
 // writes (max, sum, o[d]) per query head to the workspace and a second kernel
 // combines them in slot order.  Where one workgroup takes the whole head, a
-// short cache or one of very many heads, it writes the outputs itself.
+// short cache, one of very many heads or a sequence that is all tail, it writes
+// the outputs itself.
 //
 // The codes go to the matrix cores as bf16, which holds every int8 and e4m3
 // number exactly.  A wave takes 64 entries at a time: four 16x16x32 tiles
@@ -477,7 +478,7 @@ __global__ __launch_bounds__(ROLE == kSolo8 ? 2 * kThreads : kThreads,
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = some ? fmaf(ow[e], c, o[e]) : o[e];
     }
-    if (SOLO) {
+    if (SOLO || whole == 0) {
       f32x4 r;
 #pragma unroll
       for (int e = 0; e < 4; ++e) r[e] = l == 0.f ? 0.f : o[e] / l;
@@ -537,6 +538,7 @@ __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int 
   const uint32_t head = qh / (uint32_t)a.G, g = qh % (uint32_t)a.G;
   const int len = entries_of(a.n, head, a.hkv);
   const int whole = len > 0 ? len >> a.block_shift << a.block_shift : 0;
+  if (whole == 0) return;                               // the tail alone: its workgroup wrote the outputs
   const int chunk = chunk_of(a, whole);
   const int slots = 1 + (whole + chunk - 1) / chunk;    // the tail's and those of the splits that had entries
   const float2* ml = a.part_ml + (size_t)head * a.slots * a.G + g;
@@ -555,7 +557,7 @@ __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int 
     float M = m;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (s0 + u * SUB >= slots) v[u].x = kNegInf;     // the last slot again: weight 0
+      if (s0 + u * SUB >= slots) v[u].x = kNegInf;     // the last slot again, of codes: finite outputs of weight 0
       M = fmaxf(M, v[u].x);
     }
     const float c = weight_of(m, M);
