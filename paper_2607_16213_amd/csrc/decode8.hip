@@ -455,7 +455,8 @@ __global__ __launch_bounds__(ROLE == kSolo8 ? 2 * kThreads : kThreads,
     const int at = SOLO ? kWaves + w : w;
     const int per_wave = 4 * TailRows<T, D>::U;
     const size_t row0 = (size_t)head << shift;
-    if (lane < kMaxG) s_m[at][lane] = kNegInf;   // of the heads that the wave does not take
+    // the heads that the wave does not take: no lane of it stores their maximum again below
+    if (lane < kMaxG && lane / kTailG != g0 / kTailG) s_m[at][lane] = kNegInf;
     attend_tail<T, D>(qh + (size_t)g0 * RB, a.c.k_tail + row0 * RB, a.c.v_tail + row0 * RB,
                       APP ? a.k_new + (size_t)head * RB : nullptr, APP ? a.v_new + (size_t)head * RB : nullptr,
                       bh ? bh + whole : nullptr, active ? rest + (APP ? 1 : 0) : 0, APP ? rest : -1, a.scale,
