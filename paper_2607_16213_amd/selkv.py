@@ -589,9 +589,10 @@ class Compressor:
         """Write the compressed cache of the last run into an 8-bit cache from its start (it then holds m entries);
         bias_out [B, H, capacity], if given, gets the biases of those entries."""
         p = self.p
-        cache8_write(p, cache, self.K_out, self.V_out, 0, stream=stream)
         if bias_out is not None:
             _dev(bias_out, (p.batch, p.n_heads_kv, cache.capacity), _F32, "bias")
+        cache8_write(p, cache, self.K_out, self.V_out, 0, stream=stream)
+        if bias_out is not None:
             with torch.cuda.stream(stream):   # the current stream where none is given
                 bias_out[:, :, :self.m].copy_(self.bias)
         return cache
