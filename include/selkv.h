@@ -387,9 +387,11 @@ SELKV_API selkv_status selkv_decode_append(const selkv_params* p, const void* q,
  * largest magnitude of the block's T*d finite elements and top = 127 (int8)
  * or 448 (e4m3):
  *   scale = a / top,  code = round-to-nearest-even(x * (top / a)),  value = code * scale,
- * the divisions and the product in fp32.  A block with a < 2^-100 is stored
- * as zeros with scale 0.  An infinite element gets the code +-top, a NaN the
- * code 0: neither changes what its neighbours are stored as.
+ * the divisions and the product in fp32.  A block with a < 2^-100 (all of its
+ * finite elements are that small, or none is finite) is stored as zeros with
+ * scale 0, infinite elements too.  In any other block an infinite element
+ * gets the code +-top; a NaN gets the code 0 everywhere.  Neither changes what
+ * its neighbours are stored as.
  *
  * The open block.  Only whole blocks are quantised, each once, when its last
  * row arrives.  The rows of the last, incomplete block stay in the storage
@@ -443,6 +445,8 @@ SELKV_API void selkv_cache8_init(selkv_cache8* c);
  *      cache_len + n_new <= capacity where counts and lens are NULL.
  * In/out: the cache.  Entries in front of lens[b] and buffers behind the new
  *      entries keep their contents.
+ * Biases are the caller's: the call touches none, so before a decode with
+ *      biases the caller sets those of the new entries (0 for plain rows).
  * Workspace: none. */
 SELKV_API selkv_status selkv_cache8_write(const selkv_params* p, const selkv_cache8* c, const void* K_new,
                                           const void* V_new, int32_t n_new, int32_t cache_len, const int32_t* lens,
@@ -469,9 +473,10 @@ SELKV_API selkv_status selkv_decode8_workspace_size(const selkv_params* p, const
  *
  * out[b, h] = sum_e softmax_e(scale * q[b, h] . K[b, h/G, e] + bias[b, h/G, e]) V[b, h/G, e]
  * over the entries e < lens[b].  bias may be NULL (bitwise the result of a
- * zero bias); a bias of -inf masks its entry whatever the entry holds.  A
- * sequence with no entries, or none that is not masked, gives out = 0; a NaN
- * in a query, a bias or an unmasked row of the tail reaches the outputs.
+ * zero bias); a bias of -inf masks its entry whatever the entry and the query
+ * hold.  A sequence with no entries, or none that is not masked, gives
+ * out = 0; otherwise a NaN in a query, a bias or an unmasked row of the tail
+ * reaches the outputs.
  * Queries are not quantised and all sums are fp32.
  * In:  q [B, H_kv*G, d] (kv_dtype); bias [B, H_kv, capacity] fp32 or NULL;
  *      0 <= cache_len <= capacity.  Uses params batch, n_heads_kv, group

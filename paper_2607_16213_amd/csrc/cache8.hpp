@@ -3,7 +3,9 @@
 //
 // A block is T tokens of one KV head.  With a the largest magnitude of its
 // finite elements and top the largest code (127, or e4m3's 448):
-//   scale = a / top,  code = rne(clamp(x * (top / a))).
+//   scale = a / top,  code = rne(x * (top / a)).
+// An infinity is taken as +-a, a NaN as 0; a block with a < 2^-100, one without a
+// finite element other than 0 among them, gets scale 0 and codes 0 throughout.
 // K codes are rows of d bytes; V codes are tiles of 16 tokens, channel by
 // channel (byte ((t / 16) * d + c) * 16 + t % 16), so that a lane that wants a
 // channel's values for a run of tokens, as P V on the matrix cores does,

@@ -35,9 +35,12 @@
 // Bound by HBM where there is work enough: 32 x 8 heads of 25641 entries take
 // 300 us, 5.7 TB/s, the matrix cores busy 11% of the cycles and the VALU 38%
 // (the same loads without the products: 289).  What that took was three waves a
-// SIMD (369 us with two, 470 with two and the next step's loads in registers).
-// One layer, 8 heads of 25600 entries, takes 15.3 us: 13 in the splits, of which
-// 4.5 are a workgroup's start and end, and 3 in the combining kernel.
+// SIMD (369 us with two, 470 with two and the next step's loads in registers), at
+// the price of one spilled register a lane.  fp32 queries need two waves a SIMD
+// and twice the products of S, and take 303 us; d = 64 holds four waves, 159 us.
+// One layer, 8 heads of 25600 entries, takes 15.1 us: 13 in the splits, of which
+// 4.5 are a workgroup's start and end, and 3 in the combining kernel; 16.7 us
+// with fp32 queries, 11.2 at d = 64.
 #include <algorithm>
 
 #include "cache8.hpp"
@@ -50,11 +53,14 @@ constexpr int kThreads = kWaves * 64;
 constexpr int kMaxG = 8;
 constexpr int kTailG = 4;             // query heads of a pass over the tail: registers, shared with the codes' loop
 constexpr int kGroup = 64;            // entries of a wave's step; splits are whole multiples of them
-constexpr int kTargetBlocks = 768;    // a round of workgroups: three to a CU, what its registers hold
+// A round of workgroups: three to a CU, what the registers of bf16 at d = 128 hold.  The others hold two (fp32 at
+// d = 128: 32 x 8 heads of 25641 entries 303 us, with rounds of 512 363 us; one layer 16.7 and 21.5; only ragged MHA
+// steps gain by 512, 18.3 against 21.9) or four (bf16 at d = 64: 159 us, with rounds of 1024 168; one layer 11.2 and 11.8).
+constexpr int kTargetBlocks = 768;
 constexpr int kRounds = 4;
 constexpr int kMaxSplit = 512;
 constexpr int kCUs = 256;
-constexpr int kFewSlots = 8;
+constexpr int kFewSlots = 8;          // up to which a query head is combined by d/4 threads
 
 struct DecodeArgs8 {
   Cache8 c;
@@ -524,8 +530,9 @@ __global__ __launch_bounds__(ROLE == kSolo8 ? 2 * kThreads : kThreads,
 
 // Combines the partials of the query heads, in slot order.  A unit of d/4 threads takes four channels each of the
 // slots sub, sub + SUB, ... of a query head and loads kBatch of them at a time; with SUB > 1 the runs then meet in
-// LDS, in order.  SUB = 1 where a head has few slots, otherwise the whole workgroup takes one query head: 64 slots in
-// one trip to memory.  The kernel is a chain of latencies (3 - 4 us, two of them what any kernel takes), so its code
+// LDS, in order.  SUB = 1 where a head has few slots (64 x 8 heads of 2048 entries in 5 slots each 59.1 us, 61.4 with a
+// workgroup a query head), otherwise the whole workgroup takes one query head: 64 slots in one trip to memory (16 x 8
+// ragged heads of 25 slots 34.6 us, 36.1 with SUB = 1).  The kernel is a chain of latencies (3 - 4 us, two of them what any kernel takes), so its code
 // is kept short.
 template <int D, int SUB>
 __global__ __launch_bounds__(256) void decode8_reduce_kernel(DecodeArgs8 a, int qheads) {
@@ -635,7 +642,11 @@ hipError_t launch_td(int64_t heads, const DecodeArgs8& a, hipStream_t st) {
 int solo_entries(int d) { return d == 64 ? 1024 : 768; }
 
 // Most splits of one head: those that give the chip kRounds rounds of workgroups, none shorter than one step of its
-// four waves; none where the heads alone are a round.
+// four waves; none where the heads alone are a round.  That is best where they fill whole rounds (768 heads of 2048
+// entries take 77 us so and 105 in splits, of 8192 entries 308 and 369) and costs up to an eighth elsewhere: 800 heads of
+// 2048 entries 89 and 86 us, of 8192 entries 350 and 309, 1024 heads 431 and 389; lengths spread over 0 .. 8192, 768
+// heads 186 and 166 us.  Where few sequences are far longer than the rest it costs more: one of 25600 entries
+// among 95 of 1000, 8 heads each, takes 194 us, and among 94 of them, in splits, 60.
 int64_t most_splits(int64_t heads, int64_t groups) {
   if (heads >= kTargetBlocks) return 1;
   return std::max<int64_t>(1, std::min({(kRounds * kTargetBlocks + heads - 1) / heads, (groups + kWaves - 1) / kWaves,
@@ -658,8 +669,9 @@ size_t partial_bytes(int64_t heads, int64_t slots, int d, int G, size_t* ml) {
 // heads of 4096 entries take 29.4 us in 2048 workgroups, 32.8 in 768; ragged batches of up to 8100 entries, 16 x 8 heads
 // 33.9 us, 38.7 in one round and 36.4 in two, 24 x 8 heads 49 us, 53 in two and 52 in three.  (A sequence of its own
 // length is cut anew on the device, chunk_of.)  Every workgroup costs its prologue and its partials, though, so one
-// round is taken where it comes out even: 32 x 8 heads of 25641 entries take 300 us in 768 workgroups, 310 in 2304; and
-// a round that is barely exceeded is not begun: 8 heads of 25600 entries take 15.3 us in 400 workgroups, 16.6 in 800.
+// round is taken where it comes out even: 32 x 8 heads of 25641 entries take 300 us in 768 workgroups, 308 in 2304 (but
+// 16 x 8 such heads 162 and 158 us, 48 x 8 heads of 8192 entries 178 and 157: there several rounds would be better); and
+// a round that is barely exceeded is not begun: 8 heads of 25600 entries take 15.3 us in 400 workgroups, 16.7 in 800.
 Decode8Plan plan_decode8(int64_t heads, int cache_len, int d, int G, bool ragged) {
   Decode8Plan p{};
   const int64_t groups = ((int64_t)cache_len + kGroup - 1) / kGroup;

@@ -468,7 +468,8 @@ def _check_cache8(p, cache, tensors, lens, counts, stream):
 
 def cache8_write(p, cache, K_new, V_new, cache_len, lens=None, counts=None, stream=None):
     """Append rows K_new, V_new [B, H, n_new, d] behind the cache_len (or lens[b]) entries of every sequence;
-    counts [B] says how many of them each sequence gets (all n_new without it)."""
+    counts [B] says how many of them each sequence gets (all n_new without it).  The biases of the new entries are the
+    caller's to set (0 for plain rows)."""
     if K_new.dim() != 4:
         raise ValueError("K_new must have four dimensions")
     n_new = K_new.shape[2]
