@@ -1,0 +1,566 @@
+"""The calls of speculative generation over a paged cache that its performance is measured on.
+
+A program that has compressed a cache, or has only prefilled one, keeps it in pages and generates several tokens a
+step: it drafts a tree of tokens, puts their keys and values behind the cache with the rotary positions applied on the
+way, attends for all of them at once, accepts a path of the tree by the target's probabilities and keeps the rows of
+that path.  The cases are those calls through the package's public functions; where `own` is false `run` computes the
+same in elementary torch operations.
+
+The cache.  K and V are pools of pages [pages, H, page, d], biases [pages, H, page] fp32; table [B, columns] names the
+pages of a sequence in order, so that its entry e is row e % page of page table[b, e // page].  A sequence holds
+lens[b] entries; the n nodes of its tree (counts[b] of them) are the entries behind those, node i at lens[b] + i.
+
+Kinds
+  append  selkv.paged_append  rows into the pages, keys (and queries) rotated on the way
+  attn    selkv.tree_attn     attention of a tree's nodes; one node is an ordinary decode step
+  verify  selkv.tree_verify   the accepted path of a drafted tree and the token after it
+  keep    selkv.paged_keep    the rows of the accepted path, moved to the front of the tree's
+"""
+import math
+
+import torch
+
+own = False
+
+NEG_INF = float("-inf")
+
+
+def _cache_case(name, kind, B, H, G, d, page, length, nodes, dtype="bf16", ragged=False, bias=False, **more):
+    c = dict(kind=kind, B=B, H=H, G=G, d=d, page=page, length=length, nodes=nodes, dtype=dtype, ragged=ragged, bias=bias)
+    c.update(more)
+    return c if name is None else dict(c, name=name)
+
+
+def _append_case(name, B, H, G, d, page, length, nodes, rope="half", rot=None, queries=True, **more):
+    return _cache_case(name, "append", B, H, G, d, page, length, nodes, rope=rope, rot=d if rot is None else rot,
+                       queries=queries, **more)
+
+
+def _attn_case(name, B, H, G, d, page, length, nodes, tree="chain", masked=False, **more):
+    return _cache_case(name, "attn", B, H, G, d, page, length, nodes, tree=tree, masked=masked, **more)
+
+
+def _verify_case(name, B, nodes, vocab, tree="chain", dtype="fp32", draft=True, ragged=False):
+    c = dict(kind="verify", B=B, nodes=nodes, vocab=vocab, tree=tree, dtype=dtype, draft=draft, ragged=ragged)
+    return c if name is None else dict(c, name=name)
+
+
+def listed():
+    return [
+        # one token of one short sequence into its page: launches are all there is
+        _append_case("append_token_fp32", 1, 2, 2, 64, 16, 130, 1, dtype="fp32", rope="interleaved"),
+        # one layer's prompt of ordinary length behind an empty cache, queries rotated too, odd length
+        _append_case("append_prompt_8k", 1, 8, 4, 128, 64, 0, 8191),
+        # the compressed caches of a 32-layer model with their biases, keys rotated long ago
+        _append_case("append_compressed_25600", 32, 8, 4, 128, 64, 0, 25600, rope="none", queries=False, bias=True),
+        # the single-token form on the smallest cache
+        _attn_case("attn_token_fp32", 1, 2, 2, 64, 16, 130, 1, dtype="fp32"),
+        # a drafted chain over one layer of the compressed long-context cache
+        _attn_case("attn_chain_25600", 1, 8, 4, 128, 64, 25600, 5, bias=True),
+        # the largest tree over the same layer: 256 rows of each KV head
+        _attn_case("attn_tree_25600", 1, 8, 4, 128, 64, 25600, 64, tree="tree", bias=True),
+        # a serving batch of long contexts, a chain each: the largest case
+        _attn_case("attn_batch_25600", 32, 8, 4, 128, 64, 25641, 8, bias=True),
+        # a padded batch of trees: lengths and counts from zero up, masked entries, one sequence with nothing left
+        _attn_case("attn_ragged_masked", 16, 8, 8, 128, 32, 8100, 26, tree="tree", ragged=True, bias=True, masked=True),
+        # a chain of one sequence
+        _verify_case("verify_chain_32000", 1, 5, 32000),
+        # a serving batch of trees, each with its own number of nodes
+        _verify_case("verify_batch_131072", 32, 26, 131072, tree="tree", ragged=True),
+        # the accepted path of one layer
+        _cache_case("keep_layer", "keep", 1, 8, 4, 128, 64, 25600, 8, bias=True),
+        # the accepted paths of all 32 layers of a batch of four, full trees
+        _cache_case("keep_model_fp32", "keep", 128, 8, 4, 128, 32, 700, 64, dtype="fp32", ragged=True, bias=True),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["append", "append", "attn", "attn", "attn", "verify", "verify", "keep"])
+    if kind == "verify":
+        B, nodes, vocab = rng.choice([1, 1, 3, 8, 32]), _log_int(rng, 1, 64), _log_int(rng, 4000, 160000)
+        while B > 1 and B * nodes * vocab > 1.1e8:
+            B //= 2
+        return _verify_case(None, B, nodes, vocab, rng.choice(["chain", "tree", "tree"]), rng.choice(["fp32", "fp32", "bf16"]),
+                            rng.random() < 0.8, B > 1 and rng.random() < 0.5)
+    dtype = rng.choice(["bf16", "bf16", "bf16", "fp32"])
+    page = rng.choice([16, 32, 64, 64, 128, 256])
+    d = rng.choice([64, 128, 128])
+    H, G = rng.choice([(1, 16), (2, 2), (4, 7), (8, 4), (8, 4), (8, 8), (32, 1), (5, 3)])
+    B = rng.choice([1, 1, 2, 5, 16, 32])
+    most = 4e8 if dtype == "bf16" else 2e8
+    if kind == "append":
+        length, nodes = rng.choice([0, _log_int(rng, 1, 60000)]), _log_int(rng, 1, 25600)
+        while B > 1 and B * H * (length + nodes * (1 + G)) * d > most:
+            B //= 2
+        nodes = max(1, min(nodes, int(most / (B * H * d * (1 + G)))))
+        rope = rng.choice(["half", "interleaved", "half", "none"])
+        return _append_case(None, B, H, G, d, page, length, nodes, rope, rng.choice([d, d, d // 2, 48]),
+                            rope != "none" and rng.random() < 0.8, dtype=dtype, ragged=B > 1 and rng.random() < 0.5,
+                            bias=rng.random() < 0.5)
+    length, nodes = _log_int(rng, 1, 102400), rng.choice([1, 2, 5, 8, 13, 26, 40, 64])
+    while B > 1 and B * H * length * d > most:
+        B //= 2
+    if kind == "keep":
+        return _cache_case(None, "keep", B, H, G, d, page, length, nodes, dtype=dtype, ragged=B > 1 and rng.random() < 0.5,
+                           bias=rng.random() < 0.5)
+    while nodes > 1 and B * H * G * nodes * length * d > (2.5e10 if dtype == "bf16" else 1e10):
+        nodes //= 2
+    return _attn_case(None, B, H, G, d, page, length, nodes, rng.choice(["chain", "tree"]), rng.random() < 0.3, dtype=dtype,
+                      ragged=B > 1 and rng.random() < 0.6, bias=rng.random() < 0.7)
+
+
+def _dtype(c):
+    return torch.bfloat16 if c["dtype"] == "bf16" else torch.float32
+
+
+def _spread(most, B, at):
+    """B numbers from 0 to `most`, none, one and all of it among them, in an order that `at` turns."""
+    v = [int((0.61803398875 * (b + 1) % 1.0) * most) for b in range(B)]
+    for b, x in zip((at, at + 1, at + 2), (most, 0, min(1, most))):
+        if B > 1:
+            v[b % B] = x
+    return v
+
+
+def _lens(c):
+    return _spread(c["length"], c["B"], 1) if c["ragged"] else [c["length"]] * c["B"]
+
+
+def _counts(c):
+    return _spread(c["nodes"], c["B"], 3) if c["ragged"] else [c["nodes"]] * c["B"]
+
+
+def _paths(c):
+    """Nodes on the accepted paths of a keep case."""
+    return [min(n, 1 + (b * 5 + 2) % 7) for b, n in enumerate(_counts(c))]
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _trees(c, g):
+    """The parents of the nodes, -1 at the root; a tree's are earlier nodes, drawn, most of them near ones."""
+    B, n = c["B"], c["nodes"]
+    at = torch.arange(n, device="cuda").expand(B, n)
+    if c["tree"] == "chain":
+        parent = at - 1
+    else:
+        parent = torch.minimum((at * torch.rand((B, n), generator=g, device="cuda").sqrt()).long(), at - 1)
+    return parent.to(torch.int32).contiguous()
+
+
+def prepare(case, seed):
+    c, dev = case, "cuda"
+    g = _gen(seed)
+    if c["kind"] == "verify":
+        return _prepare_verify(c, g)
+    B, H, G, d, page, n = c["B"], c["H"], c["G"], c["d"], c["page"], c["nodes"]
+    dt = _dtype(c)
+    columns = -(-(c["length"] + n) // page) + 1
+    need = torch.tensor([-(-(x + n) // page) for x in _lens(c)], device=dev)
+    first = need.cumsum(0) - need
+    pages = int(need.sum()) + 3
+    place = torch.rand((pages,), generator=g, device=dev).argsort()
+    at = torch.arange(columns, device=dev)
+    table = torch.where(at < need[:, None], place[(first[:, None] + at).clamp(max=pages - 1)], -1).to(torch.int32)
+    channel = torch.where(torch.rand((d,), generator=g, device=dev) < 1 / 16, 4.0, 1.0)
+    s = dict(case=c, table=table, K=torch.empty((pages, H, page, d), dtype=dt, device=dev),
+             V=torch.empty((pages, H, page, d), dtype=dt, device=dev), bias=None, lens=None, counts=None)
+    some = max(1, int(1e8 / (H * page * d)))
+    for p0 in range(0, pages, some):
+        shape = s["K"][p0:p0 + some].shape
+        s["K"][p0:p0 + some] = torch.randn(shape, generator=g, device=dev).mul_(channel)
+        s["V"][p0:p0 + some] = torch.randn(shape, generator=g, device=dev)
+    if c["bias"] or c.get("masked"):   # alpha ln R: most slots absorbed nothing, the others a few times their own mass
+        u = torch.rand((pages, H, page), generator=g, device=dev)
+        s["bias"] = torch.where(u < 0.15, 0.5 * torch.log1p(40.0 * u), torch.zeros_like(u))
+        if c.get("masked"):
+            s["bias"][u > 0.9] = NEG_INF
+            if B > 1:
+                s["bias"][table[B // 2, :int(need[B // 2])].long()] = NEG_INF
+    if c["ragged"]:
+        s["lens"] = torch.tensor(_lens(c), dtype=torch.int32, device=dev)
+        s["counts"] = torch.tensor(_counts(c), dtype=torch.int32, device=dev)
+    if c["kind"] == "append":
+        # as a fused projection leaves them: token by token, queries, keys and values side by side; a compressed
+        # cache comes head by head
+        wide = H * (G + 2) if c["queries"] else 2 * H
+        rows = torch.empty((B, n, wide, d) if c["rope"] != "none" else (B, wide, n, d), dtype=dt, device=dev)
+        for b in range(B):
+            rows[b] = torch.randn(rows.shape[1:], generator=g, device=dev)
+        rows = rows if c["rope"] != "none" else rows.transpose(1, 2)
+        s["q"] = rows[:, :, :H * G] if c["queries"] else None
+        s["q_out"] = torch.zeros((B, n, H * G, d), dtype=dt, device=dev) if c["queries"] else None
+        s["k_new"], s["v_new"] = rows[:, :, -2 * H:-H], rows[:, :, -H:]
+        s["bias_new"] = 0.5 * torch.log1p(3.0 * torch.rand((B, H, n), generator=g, device=dev)) if c["bias"] else None
+        # the cache is shorter than the text where it was compressed: positions are given
+        s["positions"] = (torch.arange(n, device=dev) + 3 * torch.tensor(_lens(c), device=dev)[:, None]).to(torch.int32)
+        j = torch.arange(c["rot"] // 2, dtype=torch.float64, device=dev)
+        s["freq"] = 500000.0 ** (-2.0 * j / c["rot"]) / (1.0 + 3.0 * j / c["rot"])   # low frequencies stretched for long texts
+    elif c["kind"] == "attn":
+        s["q"] = torch.randn((B, n, H * G, d), generator=g, device=dev).to(dt)
+        s["out"] = torch.zeros_like(s["q"])
+        s["parent"] = _trees(c, g)
+    else:
+        key = torch.rand((B, n), generator=g, device=dev)
+        key[:, 0] = -1.0
+        k = torch.tensor(_paths(c), device=dev)
+        counts = torch.tensor(_counts(c), device=dev)
+        at = torch.arange(n, device=dev)
+        key = torch.where(at < counts[:, None], key, 2.0)
+        chosen = torch.where(at < k[:, None], key.argsort(1), n).sort(1).values
+        s["path"] = torch.where(at < k[:, None], chosen, -1).to(torch.int32)
+        s["n_path"] = k.to(torch.int32)
+    if own:
+        from paper_2607_16213_amd import selkv
+        s["p"] = selkv.params(batch=B, n_heads_kv=H, group=G, head_dim=d, kv_dtype=c["dtype"])
+        s["cache"] = selkv.PagedCache.over(s["p"], s["K"], s["V"], s["table"], s["bias"])
+        if c["kind"] == "append" and c["rope"] != "none":
+            s["rope"] = selkv.Rope(s["freq"], c["rope"], 1.1)
+        if c["kind"] == "attn":
+            s["ws"] = selkv.tree_workspace(s["p"], s["cache"], n)
+    return s
+
+
+def _prepare_verify(c, g):
+    B, n, V, dt, dev = c["B"], c["nodes"], c["vocab"], _dtype(c), "cuda"
+    s = dict(case=c, parent=_trees(c, g), u=torch.rand((B, n), generator=g, device=dev))
+    s["target"], draft = torch.empty((B, n, V), dtype=dt, device=dev), torch.empty((B, n, V), dtype=dt, device=dev)
+    for b in range(B):   # few likely tokens and a long tail; the draft is the target, seen through noise
+        x = torch.log(torch.rand((n, V), generator=g, device=dev) * V + 1.0).mul_(-0.9)
+        s["target"][b] = torch.softmax(x, -1)
+        draft[b] = torch.softmax(x.add_(torch.randn((n, V), generator=g, device=dev), alpha=0.7), -1)
+    bi = torch.arange(B, device=dev)
+    s["tokens"] = torch.zeros((B, n), dtype=torch.int32, device=dev)
+    for i in range(1, n):
+        cum = draft[bi, s["parent"][:, i].long()].double().cumsum(-1)
+        u = torch.rand((B, 1), generator=g, device=dev).double() * cum[:, -1:]
+        s["tokens"][:, i] = torch.searchsorted(cum, u, right=True).clamp(max=V - 1)[:, 0]
+    s["draft"] = draft if c["draft"] else None
+    s["counts"] = torch.tensor(_counts(c), dtype=torch.int32, device=dev) if c["ragged"] else None
+    s["path"] = torch.zeros((B, n), dtype=torch.int32, device=dev)
+    s["n_path"], s["next"] = (torch.zeros((B,), dtype=torch.int32, device=dev) for _ in range(2))
+    if own:
+        from paper_2607_16213_amd import selkv
+        s["ws"] = selkv.tree_verify_workspace(B, n, V, dev)
+    return s
+
+
+def run(state):
+    s, c = state, state["case"]
+    if own:
+        return _run_own(s, c)
+    if c["kind"] == "append":
+        return _plain_append(s, c)
+    if c["kind"] == "attn":
+        return {"out": _plain_attn(s, c)}
+    if c["kind"] == "verify":
+        return _plain_verify(s, c)
+    return _plain_keep(s, c)
+
+
+def _run_own(s, c):
+    from paper_2607_16213_amd import selkv
+    if c["kind"] == "append":
+        selkv.paged_append(s["p"], s["cache"], s["k_new"], s["v_new"], c["length"], lens=s["lens"], counts=s["counts"],
+                           bias_new=s["bias_new"], rope=s.get("rope"), positions=s["positions"] if "rope" in s else None,
+                           q=s["q"] if "rope" in s else None, q_out=s["q_out"] if "rope" in s else None)
+        return {"K": s["K"], "V": s["V"], "bias": s["bias"], "q_out": s["q_out"]}
+    if c["kind"] == "attn":
+        selkv.tree_attn(s["p"], s["cache"], s["q"], s["parent"], c["length"], s["out"], s["ws"], lens=s["lens"],
+                        counts=s["counts"])
+        return {"out": s["out"]}
+    if c["kind"] == "verify":
+        selkv.tree_verify(s["tokens"], s["parent"], s["target"], s["draft"], s["u"], s["path"], s["n_path"], s["next"],
+                          s["ws"], counts=s["counts"])
+        return {"path": s["path"], "n_path": s["n_path"], "next": s["next"]}
+    selkv.paged_keep(s["p"], s["cache"], s["path"], s["n_path"], c["length"], lens=s["lens"])
+    return {"K": s["K"], "V": s["V"], "bias": s["bias"]}
+
+
+def _of(c, s):
+    """Lengths and counts as tensors [B, 1]."""
+    full = lambda x: torch.full((c["B"],), x, device="cuda")
+    lens = s["lens"].long() if s["lens"] is not None else full(c["length"])
+    counts = s["counts"].long() if s["counts"] is not None else full(c["nodes"])
+    return lens[:, None], counts[:, None]
+
+
+def _slots(c, s, entry):
+    """Pages and rows of entries [B, n]."""
+    column = (entry // c["page"]).clamp(max=s["table"].shape[1] - 1)
+    return s["table"].gather(1, column).long(), entry % c["page"]
+
+
+def _rotate(x, s, c):
+    """Rows [B, n, h, d] turned by their positions, in fp32 with angles in 64 bits."""
+    r, angle = c["rot"], s["positions"].double()[..., None] * s["freq"]
+    cos, sin = (angle.cos() * 1.1).float()[:, :, None], (angle.sin() * 1.1).float()[:, :, None]
+    y = x.float()
+    a, b = (y[..., :r // 2], y[..., r // 2:r]) if c["rope"] == "half" else (y[..., 0:r:2], y[..., 1:r:2])
+    turned = (a * cos - b * sin, b * cos + a * sin)
+    turned = torch.cat(turned, -1) if c["rope"] == "half" else torch.stack(turned, -1).flatten(-2)
+    return torch.cat((turned, y[..., r:]), -1).to(x.dtype)
+
+
+def _plain_append(s, c):
+    lens, counts = _of(c, s)
+    at = torch.arange(c["nodes"], device="cuda")
+    pg, row = _slots(c, s, lens + at)
+    there = (at < counts)[..., None, None]
+    k, q = s["k_new"], s["q"]
+    if c["rope"] != "none":
+        k = _rotate(k, s, c)
+        if q is not None:
+            s["q_out"].copy_(torch.where(there, _rotate(q, s, c), s["q_out"]))
+    s["K"][pg, :, row] = torch.where(there, k, s["K"][pg, :, row])
+    s["V"][pg, :, row] = torch.where(there, s["v_new"], s["V"][pg, :, row])
+    if s["bias"] is not None:
+        s["bias"][pg, :, row] = torch.where(there[..., 0], s["bias_new"].transpose(1, 2), s["bias"][pg, :, row])
+    return {"K": s["K"], "V": s["V"], "bias": s["bias"], "q_out": s["q_out"]}
+
+
+def _ancestors(parent):
+    """[B, n, n]: whether node j is node i or above it."""
+    n = parent.shape[1]
+    up = torch.eye(n, device=parent.device) + (parent[..., None] == torch.arange(n, device=parent.device)).float()
+    for _ in range(6):
+        up = torch.matmul(up, up).clamp_(max=1.0)
+    return up > 0
+
+
+def _plain_attn(s, c):
+    """softmax(q k / sqrt(d) + bias) v over the cache and the nodes above, the node itself among them."""
+    B, H, G, d, n = c["B"], c["H"], c["G"], c["d"], c["nodes"]
+    lens, counts = _of(c, s)
+    pg = s["table"].clamp(min=0).long()
+    K, V = (x[pg].transpose(1, 2).flatten(2, 3).float() for x in (s["K"], s["V"]))       # [B, H, cap, d]
+    q = s["q"].float().view(B, n, H, G, d).transpose(1, 2).reshape(B, H, n * G, d)
+    x = torch.matmul(q, K.transpose(2, 3)).div_(math.sqrt(d)).view(B, H, n, G, -1)
+    if s["bias"] is not None:
+        x += s["bias"][pg].transpose(1, 2).flatten(2, 3)[:, :, None, None]
+    entry = torch.arange(x.shape[-1], device=x.device)
+    node = (entry - lens).clamp(0, n - 1)
+    above = _ancestors(s["parent"]).gather(2, node[:, None].expand(B, n, -1))            # [B, n, cap]
+    seen = (entry < lens)[:, None] | (above & ((entry >= lens) & (entry < lens + counts))[:, None])
+    x.masked_fill_(~seen[:, None, :, None], NEG_INF)
+    m = x.amax(-1, keepdim=True)
+    e = torch.exp(x - torch.where(m == NEG_INF, torch.zeros_like(m), m))
+    total = e.sum(-1, keepdim=True)
+    o = torch.matmul(e.view(B, H, n * G, -1), V).view(B, H, n, G, d) / total
+    o = torch.where(total > 0, o, torch.zeros_like(o)).transpose(1, 2).reshape(B, n, H * G, d)
+    there = torch.arange(n, device=x.device) < counts
+    return torch.where(there[..., None, None], o.to(s["out"].dtype), s["out"])
+
+
+def _plain_verify(s, c):
+    """The walk down the tree, node by node in order: a node is tried when its parent is where the walk stands.  With a
+    draft q it is accepted with probability r(x) / q(x), r the target's p or what the rejected siblings leave of it,
+    r = max(p - c q, 0) / S; without, a rejected token is taken out of p."""
+    B, n, V = c["B"], c["nodes"], c["vocab"]
+    dev, bi = "cuda", torch.arange(c["B"], device="cuda")
+    counts = s["counts"].long() if s["counts"] is not None else torch.full((B,), n, device=dev)
+    at = torch.zeros((B,), dtype=torch.long, device=dev)
+    used, mass = (torch.full((B,), x, dtype=torch.float64, device=dev) for x in (0.0, 1.0))
+    out = torch.zeros((B, V), dtype=torch.bool, device=dev)                              # tokens tried here in vain
+    path = torch.where((torch.arange(n, device=dev) == 0) & (counts > 0)[:, None], 0, -1)
+    length = (counts > 0).long()
+    left = lambda: (s["target"][bi, at].double() - used[:, None] * s["draft"][bi, at].double()).clamp(min=0.0)
+    for i in range(1, n):
+        x = s["tokens"][:, i].long()
+        tried = (s["parent"][:, i] == at) & (i < counts)
+        p, u = s["target"][bi, at, x].double(), s["u"][:, i].double()
+        if c["draft"]:
+            q = s["draft"][bi, at, x].double()
+            taken = tried & (u * q * mass < (p - used * q).clamp(min=0.0))
+        else:
+            p = torch.where(out[bi, x], torch.zeros_like(p), p)
+            taken = tried & (u * mass < p)
+        refused = tried & ~taken
+        if c["draft"]:
+            used = torch.where(refused, used + mass, used)
+            mass = torch.where(refused, left().sum(-1), mass)
+        else:
+            mass = torch.where(refused, mass - p, mass)
+            out[bi, x] |= refused
+        path[bi, length.clamp(max=n - 1)] = torch.where(taken, i, path[bi, length.clamp(max=n - 1)])
+        length = length + taken.long()
+        at = torch.where(taken, i, at)
+        used, mass = torch.where(taken, 0.0, used), torch.where(taken, 1.0, mass)
+        out &= ~taken[:, None]
+    w = left() if c["draft"] else s["target"][bi, at].double().masked_fill(out, 0.0)
+    w = torch.where(w.sum(-1, keepdim=True) > 0, w, s["target"][bi, at].double())
+    cum = w.cumsum(-1)
+    token = torch.searchsorted(cum, s["u"][:, :1].double() * cum[:, -1:], right=True)[:, 0].clamp(max=V - 1)
+    nxt = torch.where(counts > 0, token, -1)
+    return {"path": path.to(torch.int32), "n_path": length.to(torch.int32), "next": nxt.to(torch.int32)}
+
+
+def _plain_keep(s, c):
+    lens, _ = _of(c, s)
+    at = torch.arange(c["nodes"], device="cuda")
+    kept = at < s["n_path"].long()[:, None]
+    src = _slots(c, s, lens + torch.where(kept, s["path"].long(), at))
+    dst = _slots(c, s, lens + at)
+    for x in (s["K"], s["V"], s["bias"]):
+        if x is not None:
+            x[dst[0], :, dst[1]] = x[src[0], :, src[1]]
+    return {"K": s["K"], "V": s["V"], "bias": s["bias"]}
+
+
+def work(case):
+    c = case
+    if c["kind"] == "verify":
+        # the rows that the last token is drawn from, and the nodes
+        rows, esz = 2 if c["draft"] else 1, 2 if c["dtype"] == "bf16" else 4
+        live = sum(1 for n in _counts(c) if n)
+        return {"bytes": float(live * rows * c["vocab"] * esz + 16 * sum(_counts(c))), "flops": 4.0 * live * c["vocab"]}
+    H, G, d, esz = c["H"], c["G"], c["d"], 2 if c["dtype"] == "bf16" else 4
+    if c["kind"] == "append":
+        rows = sum(_counts(c)) * H
+        turned = rows * ((1 + G if c["queries"] else 1) * c["rot"] if c["rope"] != "none" else 0)
+        per = (2 + (G if c["queries"] and c["rope"] != "none" else 0)) * 2 * d * esz + (8 if c["bias"] else 0)
+        return {"bytes": float(rows * per), "flops": 3.0 * turned}
+    if c["kind"] == "keep":
+        rows = sum(max(0, k - 1) for k in _paths(c)) * H
+        return {"bytes": float(rows * (4 * d * esz + (8 if c["bias"] else 0)) + 4 * sum(_counts(c))), "flops": 0.0}
+    b = f = 0
+    for n, k in zip(_lens(c), _counts(c)):
+        if k:
+            b += (n + k) * (2 * d * esz + (4 if c["bias"] or c["masked"] else 0)) + 2 * k * G * d * esz
+            f += 4 * G * k * (n + k) * d
+    return {"bytes": float(H * b), "flops": float(H * f)}
+
+
+def exact(case, seed):
+    c = case
+    s = prepare(c, seed)
+    if c["kind"] == "append":
+        return _exact_append(c, s)
+    if c["kind"] == "attn":
+        return {"out": _exact_attn(c, s)}
+    if c["kind"] == "verify":
+        return _exact_verify(c, s)
+    return _exact_keep(c, s)
+
+
+def _places(c, s, b, first, count):
+    """Pages and rows of entries first .. first + count - 1 of a sequence."""
+    e = torch.arange(first, first + count, device="cuda")
+    return s["table"][b].long()[e // c["page"]], e % c["page"]
+
+
+def _exact_turn(c, s, x, b):
+    """Rows [m, h, d] of sequence b as complex numbers times scale * e^(i angle)."""
+    if c["rope"] == "none":
+        return x.double()
+    m, r = x.shape[0], c["rot"]
+    y = x.double()
+    half = c["rope"] == "half"
+    z = torch.complex(y[..., :r // 2], y[..., r // 2:r]) if half else torch.view_as_complex(y[..., :r].unflatten(-1, (-1, 2)).contiguous())
+    a = s["positions"][b, :m].double()[:, None] * s["freq"][None]
+    z = z * torch.polar(torch.full_like(a, 1.1), a)[:, None]
+    turned = torch.cat((z.real, z.imag), -1) if half else torch.view_as_real(z).flatten(-2)
+    return torch.cat((turned, y[..., r:]), -1)
+
+
+def _exact_append(c, s):
+    K = s["K"].double() if c["rope"] != "none" else s["K"].clone()
+    V, bias = s["V"].clone(), None if s["bias"] is None else s["bias"].clone()
+    q = None if s["q_out"] is None else s["q_out"].double()
+    for b, (n, k) in enumerate(zip(_lens(c), _counts(c))):
+        if k == 0:
+            continue
+        pg, row = _places(c, s, b, n, k)
+        K[pg, :, row] = _exact_turn(c, s, s["k_new"][b, :k], b).to(K.dtype)
+        V[pg, :, row] = s["v_new"][b, :k]
+        if bias is not None:
+            bias[pg, :, row] = s["bias_new"][b, :, :k].t()
+        if q is not None and c["rope"] != "none":
+            q[b, :k] = _exact_turn(c, s, s["q"][b, :k], b)
+    return {"K": K, "V": V, "bias": bias, "q_out": q}
+
+
+def _exact_attn(c, s):
+    B, H, G, d, n = c["B"], c["H"], c["G"], c["d"], c["nodes"]
+    out = s["out"].double()
+    parents = s["parent"].cpu().tolist()
+    for b, (have, k) in enumerate(zip(_lens(c), _counts(c))):
+        if k == 0:
+            continue
+        pg, row = _places(c, s, b, 0, have + k)
+        hidden = torch.ones((k, k), dtype=torch.bool)
+        for i in range(k):
+            j = i
+            while j >= 0:
+                hidden[i, j] = False
+                j = parents[b][j]
+        hidden = hidden.cuda().repeat_interleave(G, 0)
+        for h in range(H):
+            keys, values = s["K"][pg, h, row].double(), s["V"][pg, h, row].double()
+            x = (s["q"][b, :k, h * G:(h + 1) * G].reshape(k * G, d).double() @ keys.t().contiguous()) * d ** -0.5
+            if s["bias"] is not None:
+                x += s["bias"][pg, h, row].double()
+            x[:, have:] = x[:, have:].masked_fill(hidden, NEG_INF)
+            w = torch.softmax(x, -1)
+            w = torch.where(torch.isnan(w), 0.0, w)      # a row with nothing left
+            out[b, :k, h * G:(h + 1) * G] = (w @ values).view(k, G, d)
+    return out
+
+
+def _exact_verify(c, s):
+    """The same walk with the residual distribution itself, normalised after every refusal."""
+    n = c["nodes"]
+    path = torch.full((c["B"], n), -1, dtype=torch.int32)
+    length, nxt = torch.zeros(c["B"], dtype=torch.int32), torch.full((c["B"],), -1, dtype=torch.int32)
+    tokens, parents, us = s["tokens"].tolist(), s["parent"].tolist(), s["u"].double().tolist()
+    for b, k in enumerate(_counts(c)):
+        if k == 0:
+            continue
+        at, taken = 0, [0]
+        while True:
+            target, r = s["target"][b, at].double(), s["target"][b, at].double()
+            q = s["draft"][b, at].double() if c["draft"] else None
+            mass, found = 1.0, None
+            for i in [i for i in range(1, k) if parents[b][i] == at]:
+                x = tokens[b][i]
+                if us[b][i] * (float(q[x]) if c["draft"] else mass) < float(r[x]):
+                    found = i
+                    break
+                if c["draft"]:
+                    r = torch.relu(r - q)
+                    r = r / r.sum()
+                else:
+                    mass -= float(r[x])
+                    r = r.clone()
+                    r[x] = 0.0
+            if found is None:
+                break
+            at = found
+            taken.append(found)
+        total = float(r.sum())
+        r = r if total > 0.0 else target
+        cum = torch.cumsum(r, 0)
+        path[b, :len(taken)] = torch.tensor(taken, dtype=torch.int32)
+        length[b], nxt[b] = len(taken), int((cum <= us[b][0] * cum[-1]).sum().clamp(max=c["vocab"] - 1))
+    return {"path": path.cuda(), "n_path": length.cuda(), "next": nxt.cuda()}
+
+
+def _exact_keep(c, s):
+    got = {k: None if s[k] is None else s[k].clone() for k in ("K", "V", "bias")}
+    for b, (n, k) in enumerate(zip(_lens(c), _paths(c))):
+        if k == 0:
+            continue
+        pg, row = _places(c, s, b, n, c["nodes"])
+        src = s["path"][b, :k].long()
+        for x in got:
+            if got[x] is not None:
+                got[x][pg[:k], :, row[:k]] = s[x][pg[src], :, row[src]]
+    return got
