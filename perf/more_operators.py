@@ -388,7 +388,7 @@ def _plain_verify(s, c):
             used = torch.where(refused, used + mass, used)
             mass = torch.where(refused, left().sum(-1), mass)
         else:
-            mass = torch.where(refused, mass - p, mass)
+            mass = torch.where(refused, (mass - p).clamp(min=0.0), mass)
             out[bi, x] |= refused
         path[bi, length.clamp(max=n - 1)] = torch.where(taken, i, path[bi, length.clamp(max=n - 1)])
         length = length + taken.long()
@@ -538,7 +538,7 @@ def _exact_verify(c, s):
                     r = torch.relu(r - q)
                     r = r / r.sum()
                 else:
-                    mass -= float(r[x])
+                    mass = max(mass - float(r[x]), 0.0)
                     r = r.clone()
                     r[x] = 0.0
             if found is None:
