@@ -503,6 +503,187 @@ SELKV_API selkv_status selkv_decode8_append(const selkv_params* p, const selkv_c
                                             const int32_t* lens, float* out, void* ws, size_t ws_bytes,
                                             hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * A cache in pages, and trees of drafted tokens
+ *
+ * A cache (compressed or not) whose sequences own pages of a common pool, and
+ * the calls of a generation step that takes several drafted tokens at once:
+ * selkv_paged_append stores their keys and values, selkv_tree_attn attends for
+ * all of them, selkv_tree_verify accepts a path of them, selkv_paged_keep
+ * keeps the rows of that path.
+ *
+ * Pages.  Entry e of sequence b is row e % page of page table[b, e / page], in
+ * the pools of K, of V and (if there is one) of the biases.  A column past the
+ * table or an id outside [0, n_pages), -1 say, is no page: rows for it are not
+ * stored and entries on it are left out.  Pages may be shared by sequences as
+ * long as no call stores into them.
+ *
+ * Trees.  The n <= 64 nodes of a sequence are drafted tokens; node 0 is the
+ * root, the last token that is certain, whose key and value the cache does not
+ * hold yet.  parent [B, n] (int32, on the device) names every node's parent,
+ * an earlier node; any other value makes the node a root of its own, which
+ * attends to the cache and itself and which selkv_tree_verify never reaches.
+ * parent = NULL: a chain, node i - 1 above node i.  One node is an ordinary
+ * decode step.  While a tree is tried its rows are the entries behind those of
+ * the sequence: node i is entry lens[b] + i.
+ *
+ * Lengths.  As for the 8-bit cache: lens = NULL means that every sequence
+ * holds cache_len entries, otherwise lens[b] (int32, on the device) counts
+ * them and cache_len is an upper bound.  counts = NULL means n rows or nodes
+ * for every sequence, otherwise counts[b] (int32, on the device) of them.  The
+ * library only reads both.  A sequence whose lens[b] is outside [0, cache_len]
+ * or whose counts[b] is outside [0, n] takes no part: nothing of it is read or
+ * stored, and what the call writes for its rows is left as it was, as it is for
+ * rows from counts[b] on.
+ * ------------------------------------------------------------------------- */
+
+/* A paged cache: its sizes and the caller's device buffers.  H_kv, d, B and the
+ * storage type come from selkv_params. */
+typedef struct selkv_paged {
+  uint32_t struct_size;  /* = sizeof(selkv_paged) */
+  int32_t page;          /* entries of a page: 16, 32, 64, 128 or 256 (default 64) */
+  int32_t n_pages;       /* pages of the pool, at most 2^28 / page */
+  int32_t columns;       /* pages a sequence can have; columns * page is its capacity, at most 2^28 */
+  void* K;               /* [n_pages, H_kv, page, d] in kv_dtype */
+  void* V;               /* [n_pages, H_kv, page, d] in kv_dtype */
+  float* bias;           /* [n_pages, H_kv, page], 16-byte aligned, or NULL: all biases are 0 */
+  const int32_t* table;  /* [B, columns] */
+} selkv_paged;
+
+/* Fill `c` with the defaults: page = 64, sizes 0 and NULL pointers (to be set). */
+SELKV_API void selkv_paged_init(selkv_paged* c);
+
+/* Rows [B, n, heads, d] of an input, d elements side by side, the other strides
+ * as given: a slice of a fused projection, or rows stored head by head. */
+typedef struct selkv_rows {
+  const void* data;                      /* 16-byte aligned */
+  int64_t stride_b, stride_n, stride_h;  /* in elements; not negative, multiples of 16 bytes */
+} selkv_rows;
+
+typedef enum selkv_rope_layout {
+  SELKV_ROPE_HALF = 0,        /* channel j turns with channel j + rot_dim / 2 */
+  SELKV_ROPE_INTERLEAVED = 1  /* channel 2 j with channel 2 j + 1 */
+} selkv_rope_layout;
+
+/* Rotary positions.  Of a row's first rot_dim channels pair j turns by the angle
+ * a = position * freq[j] radians, (x, y) -> scale (x cos a - y sin a, y cos a +
+ * x sin a); the other channels stay.  freq holds whatever the model's base and
+ * its scaling for long contexts give; scale is what some of these put on the
+ * rotated part (1 otherwise).  The angle is formed and reduced in fp64, sine,
+ * cosine and the products are fp32. */
+typedef struct selkv_rope {
+  uint32_t struct_size;  /* = sizeof(selkv_rope) */
+  int32_t layout;        /* selkv_rope_layout */
+  int32_t rot_dim;       /* a multiple of 16, 16 .. d */
+  float scale;
+  const double* freq;    /* [rot_dim / 2] on the device, 8-byte aligned */
+} selkv_rope;
+
+/* Fill `r` with the defaults: HALF, scale 1, rot_dim 0 and NULL (to be set). */
+SELKV_API void selkv_rope_init(selkv_rope* r);
+
+/* Append rows to every sequence: row i of sequence b becomes entry lens[b] + i,
+ * keys (and queries) turned by their positions on the way.
+ *
+ * A prompt, a compressed cache with its biases, a chunk of a prefill, a tree of
+ * drafts or a single token.  Rows past the capacity, or for no page, are not
+ * stored.
+ * In:  k_new, v_new [B, n_new, H_kv, d] (kv_dtype; must not overlap the cache);
+ *      bias_new [B, H_kv, n_new] fp32 or NULL (zeros); rope or NULL (keys are
+ *      stored as they are); positions [B, n_new] int32 or NULL (lens[b] + i);
+ *      q [B, n_new, H_kv*G, d] or NULL, which needs rope; n_new >= 1;
+ *      cache_len + n_new at most the capacity where lens and counts are NULL.
+ * In/out: the pages of the new entries; biases where the cache has them (bias_new
+ *      needs them).
+ * Out: q_out [B, n_new, H_kv*G, d] contiguous, the turned queries; may be q's own
+ *      memory where q is laid out the same.
+ * Workspace: none. */
+SELKV_API selkv_status selkv_paged_append(const selkv_params* p, const selkv_paged* c, const selkv_rows* k_new,
+                                          const selkv_rows* v_new, const float* bias_new, const selkv_rope* rope,
+                                          const int32_t* positions, const selkv_rows* q, void* q_out, int32_t n_new,
+                                          int32_t cache_len, const int32_t* lens, const int32_t* counts,
+                                          hipStream_t stream);
+
+/* Bytes of scratch that selkv_tree_attn needs for `p`, `c` and up to `n` nodes,
+ * at every cache_len up to the capacity (of `c` only the sizes are read).
+ * Host-only. */
+SELKV_API selkv_status selkv_tree_workspace_size(const selkv_params* p, const selkv_paged* c, int32_t n,
+                                                 size_t* bytes);
+
+/* Attention of the nodes of a tree over a paged cache:
+ *
+ * out[b, i, h] = sum_e softmax_e(scale * q[b, i, h] . K[b, h/G, e] + bias[b, h/G, e]) V[b, h/G, e]
+ * over the entries e < lens[b] and the nodes on the way from node i to its
+ * root, node i included (their rows as selkv_paged_append stored them).  A bias
+ * of -inf masks its entry whatever the entry and the query hold, and no node's
+ * row reaches a node that does not attend to it; a node that nothing is left
+ * for gives 0.  Sums, maxima and logits are fp32; for bf16 the softmax weights
+ * enter the product with V as sums of two bf16 numbers.
+ * In:  q [B, n, H_kv*G, d] (kv_dtype); parent [B, n] or NULL; 1 <= n <= 64;
+ *      cache_len >= 0, and cache_len + n at most the capacity where lens and
+ *      counts are NULL.  Uses params batch, n_heads_kv, group (1..64),
+ *      head_dim, kv_dtype and scale only.
+ * Out: out [B, n, H_kv*G, d] in kv_dtype.
+ * Workspace: selkv_tree_workspace_size(); no initialisation is needed.  Calls
+ *      that may overlap in time need separate workspaces. */
+SELKV_API selkv_status selkv_tree_attn(const selkv_params* p, const selkv_paged* c, const void* q,
+                                       const int32_t* parent, int32_t n, int32_t cache_len, const int32_t* lens,
+                                       const int32_t* counts, void* out, void* ws, size_t ws_bytes,
+                                       hipStream_t stream);
+
+/* Bytes of scratch that selkv_tree_verify needs.  Host-only. */
+SELKV_API selkv_status selkv_tree_verify_workspace_size(int32_t batch, int32_t n, int32_t vocab, size_t* bytes);
+
+/* Verification of drafted tokens against the target's probabilities, from given
+ * random numbers: which path of every tree is accepted, and the token after it.
+ *
+ * target[b, i] is the target's distribution after node i, draft[b, i] the one
+ * that node i's children were drawn from, one after the other and each by
+ * itself.  A walk starts at node 0; at node v, with p = target[b, v] and q =
+ * draft[b, v], it tries the children of v in ascending order and goes on from
+ * the first that is accepted.  A child with token x is accepted with
+ * probability min(1, r(x) / q(x)), r being p at first and, after every child
+ * refused, what q leaves of it: r <- max(r - q, 0), normalised.  After k
+ * refusals that is max(p - c_k q, 0) / S_k with
+ *   c_0 = 0, S_0 = 1, c_(k+1) = c_k + S_k, S_k = sum_x max(p(x) - c_k q(x), 0),
+ * and the test is u[b, i] q(x) S_k < max(p(x) - c_k q(x), 0).  Where no child is
+ * left, the next token is drawn from r (from p if nothing is left of it): the
+ * lowest x at which the sum of the weights up to x exceeds u[b, 0] times their
+ * total.  So tokens have the target's distribution, whatever the draft's.
+ * draft = NULL: children without a distribution, each as if drawn with
+ * certainty.  Child x is accepted if u[b, i] S < p(x); refused, x is taken out of
+ * p, S (1 at first) becomes max(S - p(x), 0), and x refused once is refused again.
+ * All of this is fp64 on the probabilities as given.  A weight that is negative
+ * or NaN counts as 0 and accepts nothing; a token outside [0, vocab) is refused.
+ * In:  tokens [B, n] int32 (of node 0 it is not read); parent [B, n] int32 or
+ *      NULL; target and draft (or NULL) [B, n, vocab] in dtype (selkv_dtype);
+ *      u [B, n] fp32 in [0, 1); counts [B] int32 or NULL; 1 <= n <= 64;
+ *      1 <= vocab <= 2^21; batch <= 65535.
+ * Out: path [B, n] int32: node 0 and the accepted nodes, ascending, -1 behind
+ *      them; n_path [B] int32, their number; next [B] int32, the token after the
+ *      last of them (-1 if the target's row holds no positive probability).  A
+ *      sequence with counts[b] outside [1, n] gets n_path 0 and -1 elsewhere.
+ * Workspace: selkv_tree_verify_workspace_size(); no initialisation is needed. */
+SELKV_API selkv_status selkv_tree_verify(int32_t batch, int32_t n, int32_t vocab, int32_t dtype,
+                                         const int32_t* tokens, const int32_t* parent, const void* target,
+                                         const void* draft, const float* u, const int32_t* counts, int32_t* path,
+                                         int32_t* n_path, int32_t* next, void* ws, size_t ws_bytes,
+                                         hipStream_t stream);
+
+/* Keep the accepted path of a tree: for j < n_path[b] the row and bias of entry
+ * lens[b] + path[b, j] move to entry lens[b] + j, as if all at once.  The caller
+ * then advances lens[b] by n_path[b]; the other nodes' rows stay behind the end
+ * until they are overwritten.
+ * In:  path [B, n] and n_path [B] int32, as selkv_tree_verify writes them; a
+ *      node outside [0, n) moves nothing, a sequence with n_path[b] outside
+ *      [0, n] takes no part; 1 <= n <= 64; 0 <= cache_len, and cache_len + n at
+ *      most the capacity where lens is NULL.
+ * In/out: the pages of the entries.
+ * Workspace: none. */
+SELKV_API selkv_status selkv_paged_keep(const selkv_params* p, const selkv_paged* c, const int32_t* path,
+                                        const int32_t* n_path, int32_t n, int32_t cache_len, const int32_t* lens,
+                                        hipStream_t stream);
+
 /* Static, NUL-terminated description of a status code. */
 SELKV_API const char* selkv_status_string(selkv_status s);
 

@@ -157,4 +157,51 @@ hipError_t launch_decode8(int64_t heads, int hkv, int d, int G, int dtype, float
                           const Cache8& c, const Lens8& n, const void* q, float* bias, const void* k_new,
                           const void* v_new, float* out, void* ws, hipStream_t st);
 
+// A cache in pages as the kernels see it.
+struct Paged {
+  int shift;           // log2 of a page's entries
+  int n_pages, columns;
+  char* K;
+  char* V;
+  float* bias;
+  const int32_t* table;
+};
+
+// Lengths of the sequences (cache_len, or lens[b] up to it) and their new rows or nodes (n, or counts[b] up to it).
+struct Seqs {
+  int cache_len, n;
+  const int32_t* lens;
+  const int32_t* counts;
+};
+
+// Input rows with strides in elements.
+struct RowsIn {
+  const char* data;
+  int64_t sb, sn, sh;
+};
+
+struct TreePlan {
+  int row_tiles;       // 16-row tiles of a wave
+  bool split_rows;     // the waves of a workgroup take rows of their own, otherwise entries of their own
+  int row_blocks;      // workgroups that share a KV head's entries
+  int splits;          // workgroups along the entries
+  size_t ml_off, bytes;
+};
+
+TreePlan plan_tree(int64_t heads, int entries, int d, int rows, size_t elem);   // entries: the most a sequence can have
+size_t tree_workspace_bound(int64_t heads, int capacity, int d, int G, int n, size_t elem);
+
+hipError_t launch_paged_append(int batch, int hkv, int d, int dtype, const Paged& c, const Seqs& n, const RowsIn& k,
+                               const RowsIn& v, const float* bias_new, const selkv_rope* rope,
+                               const int32_t* positions, const RowsIn& q, int hq, void* q_out, hipStream_t st);
+hipError_t launch_paged_keep(int batch, int hkv, int d, int dtype, const Paged& c, const Seqs& n, const int32_t* path,
+                             const int32_t* n_path, hipStream_t st);
+hipError_t launch_tree_attn(int batch, int hkv, int d, int G, int dtype, float scale, const TreePlan& plan,
+                            const Paged& c, const Seqs& n, const void* q, const int32_t* parent, void* out, void* ws,
+                            hipStream_t st);
+size_t tree_verify_bytes(int batch, int n, int vocab);
+hipError_t launch_tree_verify(int batch, int n, int vocab, int dtype, const int32_t* tokens, const int32_t* parent,
+                              const void* target, const void* draft, const float* u, const int32_t* counts,
+                              int32_t* path, int32_t* n_path, int32_t* next, void* ws, hipStream_t st);
+
 }  // namespace selkv

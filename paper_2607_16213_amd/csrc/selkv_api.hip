@@ -159,6 +159,77 @@ selkv_status check_cache8(const selkv_params* p, const selkv_cache8* c, bool buf
   return SELKV_OK;
 }
 
+// A paged cache's sizes and, where `buffers`, its pointers.
+selkv_status check_paged(const selkv_params* p, const selkv_paged* c, bool buffers) {
+  if (!p || p->struct_size != sizeof(selkv_params) || !c || c->struct_size != sizeof(selkv_paged)) return SELKV_EINVAL;
+  if (p->kv_dtype != SELKV_F32 && p->kv_dtype != SELKV_BF16) return SELKV_EDTYPE;
+  if (p->batch < 1 || p->n_heads_kv < 1) return SELKV_EINVAL;
+  if (p->head_dim != 64 && p->head_dim != 128) return SELKV_EUNSUPPORTED;
+  if ((int64_t)p->batch * p->n_heads_kv > 65535) return SELKV_EUNSUPPORTED;   // grid y dimension
+  if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128 && c->page != 256) return SELKV_EUNSUPPORTED;
+  if (c->columns < 1) return SELKV_EINVAL;
+  if (c->columns > (1 << 28) / c->page) return SELKV_EUNSUPPORTED;
+  if (!buffers) return SELKV_OK;
+  if (c->n_pages < 1 || !c->K || !c->V || !c->table) return SELKV_EINVAL;
+  if (c->n_pages > (1 << 28) / c->page) return SELKV_EUNSUPPORTED;
+  if (!aligned(c->K, 16) || !aligned(c->V, 16) || !aligned(c->bias, 16) || !aligned(c->table, 4)) return SELKV_EALIGN;
+  return SELKV_OK;
+}
+
+Paged view_paged(const selkv_paged* c) {
+  return Paged{__builtin_ctz(c->page), c->n_pages, c->columns, static_cast<char*>(c->K), static_cast<char*>(c->V),
+               c->bias, c->table};
+}
+
+// n rows or nodes behind the entries of every sequence; `known`: the host knows where they end.
+selkv_status check_seqs(const selkv_paged* c, int32_t n, int32_t cache_len, bool known, const int32_t* lens,
+                        const int32_t* counts) {
+  const int32_t capacity = c->columns * c->page;
+  if (n < 1 || n > capacity || cache_len < 0 || cache_len > capacity) return SELKV_EINVAL;
+  if (known && n > capacity - cache_len) return SELKV_EINVAL;   // no room
+  if (!aligned(lens, 4) || !aligned(counts, 4)) return SELKV_EALIGN;
+  return SELKV_OK;
+}
+
+constexpr int kMaxNodes = 64;
+
+selkv_status check_tree(const selkv_params* p, const selkv_paged* c, int32_t n, bool buffers) {
+  const selkv_status st = check_paged(p, c, buffers);
+  if (st != SELKV_OK) return st;
+  if (p->group < 1 || n < 1) return SELKV_EINVAL;
+  if (p->group > 64 || n > kMaxNodes) return SELKV_EUNSUPPORTED;
+  if (!(p->scale >= 0.f) || !isfinite(p->scale)) return SELKV_EINVAL;
+  return SELKV_OK;
+}
+
+selkv_status check_rows(const selkv_params* p, const selkv_rows* r, RowsIn* out) {
+  if (!r || !r->data) return SELKV_EINVAL;
+  const int64_t unit = 16 / (int64_t)elem_size(p);
+  for (const int64_t s : {r->stride_b, r->stride_n, r->stride_h}) {
+    if (s < 0) return SELKV_EINVAL;
+    if (s % unit) return SELKV_EALIGN;
+  }
+  if (!aligned(r->data, 16)) return SELKV_EALIGN;
+  *out = RowsIn{static_cast<const char*>(r->data), r->stride_b, r->stride_n, r->stride_h};
+  return SELKV_OK;
+}
+
+selkv_status check_rope(const selkv_params* p, const selkv_rope* r) {
+  if (r->struct_size != sizeof(selkv_rope)) return SELKV_EINVAL;
+  if (r->layout != SELKV_ROPE_HALF && r->layout != SELKV_ROPE_INTERLEAVED) return SELKV_EINVAL;
+  if (r->rot_dim < 2 || r->rot_dim > p->head_dim) return SELKV_EINVAL;
+  if (r->rot_dim % 16) return SELKV_EUNSUPPORTED;
+  if (!isfinite(r->scale) || !r->freq) return SELKV_EINVAL;
+  if (!aligned(r->freq, 8)) return SELKV_EALIGN;
+  return SELKV_OK;
+}
+
+selkv_status check_verify(int32_t batch, int32_t n, int32_t vocab) {
+  if (batch < 1 || n < 1 || vocab < 1) return SELKV_EINVAL;
+  if (batch > 65535 || n > kMaxNodes || vocab > (1 << 21)) return SELKV_EUNSUPPORTED;
+  return SELKV_OK;
+}
+
 // ... and those of the two decode calls on one.
 selkv_status check_decode8(const selkv_params* p, const selkv_cache8* c, const void* q, const float* bias,
                            int32_t cache_len, const int32_t* lens, float* out) {
@@ -555,6 +626,111 @@ SELKV_API selkv_status selkv_decode8_append(const selkv_params* p, const selkv_c
   if ((st = check_ws(ws, ws_bytes, plan.bytes)) != SELKV_OK) return st;
   return hip_status(launch_decode8(heads, p->n_heads_kv, p->head_dim, p->group, p->kv_dtype, eff_scale(p), plan,
                                    view_cache8(c), Lens8{cache_len, lens}, q, bias, k_new, v_new, out, ws, stream));
+}
+
+SELKV_API void selkv_paged_init(selkv_paged* c) {
+  if (!c) return;
+  memset(c, 0, sizeof(*c));
+  c->struct_size = sizeof(selkv_paged);
+  c->page = 64;
+}
+
+SELKV_API void selkv_rope_init(selkv_rope* r) {
+  if (!r) return;
+  memset(r, 0, sizeof(*r));
+  r->struct_size = sizeof(selkv_rope);
+  r->layout = SELKV_ROPE_HALF;
+  r->scale = 1.f;
+}
+
+SELKV_API selkv_status selkv_paged_append(const selkv_params* p, const selkv_paged* c, const selkv_rows* k_new,
+                                          const selkv_rows* v_new, const float* bias_new, const selkv_rope* rope,
+                                          const int32_t* positions, const selkv_rows* q, void* q_out, int32_t n_new,
+                                          int32_t cache_len, const int32_t* lens, const int32_t* counts,
+                                          hipStream_t stream) {
+  selkv_status st = check_paged(p, c, true);
+  if (st != SELKV_OK) return st;
+  RowsIn k, v, qr = {nullptr, 0, 0, 0};
+  if ((st = check_seqs(c, n_new, cache_len, !lens && !counts, lens, counts)) != SELKV_OK) return st;
+  if ((st = check_rows(p, k_new, &k)) != SELKV_OK || (st = check_rows(p, v_new, &v)) != SELKV_OK) return st;
+  if (rope && (st = check_rope(p, rope)) != SELKV_OK) return st;
+  if (bias_new && !c->bias) return SELKV_EINVAL;
+  if (!aligned(bias_new, 4) || !aligned(positions, 4)) return SELKV_EALIGN;
+  if (q) {
+    if (!rope || !q_out || p->group < 1) return SELKV_EINVAL;
+    if (p->group > 64) return SELKV_EUNSUPPORTED;
+    if ((st = check_rows(p, q, &qr)) != SELKV_OK) return st;
+    if (!aligned(q_out, 16)) return SELKV_EALIGN;
+  }
+  return hip_status(launch_paged_append(p->batch, p->n_heads_kv, p->head_dim, p->kv_dtype, view_paged(c),
+                                        Seqs{cache_len, n_new, lens, counts}, k, v, bias_new, rope, positions, qr,
+                                        q ? p->n_heads_kv * p->group : 0, q_out, stream));
+}
+
+SELKV_API selkv_status selkv_tree_workspace_size(const selkv_params* p, const selkv_paged* c, int32_t n,
+                                                 size_t* bytes) {
+  if (!bytes) return SELKV_EINVAL;
+  const selkv_status st = check_tree(p, c, n, false);
+  if (st != SELKV_OK) return st;
+  *bytes = tree_workspace_bound((int64_t)p->batch * p->n_heads_kv, c->columns * c->page, p->head_dim, p->group, n,
+                                elem_size(p));
+  return SELKV_OK;
+}
+
+SELKV_API selkv_status selkv_tree_attn(const selkv_params* p, const selkv_paged* c, const void* q,
+                                       const int32_t* parent, int32_t n, int32_t cache_len, const int32_t* lens,
+                                       const int32_t* counts, void* out, void* ws, size_t ws_bytes,
+                                       hipStream_t stream) {
+  selkv_status st = check_tree(p, c, n, true);
+  if (st != SELKV_OK) return st;
+  if ((st = check_seqs(c, n, cache_len, !lens && !counts, lens, counts)) != SELKV_OK) return st;
+  if (!q || !out) return SELKV_EINVAL;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(parent, 4)) return SELKV_EALIGN;
+  const int32_t capacity = c->columns * c->page;
+  const int32_t entries = n > capacity - cache_len ? capacity : cache_len + n;
+  const TreePlan plan =
+      plan_tree((int64_t)p->batch * p->n_heads_kv, entries, p->head_dim, n * p->group, elem_size(p));
+  if ((st = check_ws(ws, ws_bytes, plan.bytes)) != SELKV_OK) return st;
+  return hip_status(launch_tree_attn(p->batch, p->n_heads_kv, p->head_dim, p->group, p->kv_dtype, eff_scale(p), plan,
+                                     view_paged(c), Seqs{cache_len, n, lens, counts}, q, parent, out, ws, stream));
+}
+
+SELKV_API selkv_status selkv_tree_verify_workspace_size(int32_t batch, int32_t n, int32_t vocab, size_t* bytes) {
+  if (!bytes) return SELKV_EINVAL;
+  const selkv_status st = check_verify(batch, n, vocab);
+  if (st != SELKV_OK) return st;
+  *bytes = tree_verify_bytes(batch, n, vocab);
+  return SELKV_OK;
+}
+
+SELKV_API selkv_status selkv_tree_verify(int32_t batch, int32_t n, int32_t vocab, int32_t dtype,
+                                         const int32_t* tokens, const int32_t* parent, const void* target,
+                                         const void* draft, const float* u, const int32_t* counts, int32_t* path,
+                                         int32_t* n_path, int32_t* next, void* ws, size_t ws_bytes,
+                                         hipStream_t stream) {
+  selkv_status st = check_verify(batch, n, vocab);
+  if (st != SELKV_OK) return st;
+  if (dtype != SELKV_F32 && dtype != SELKV_BF16) return SELKV_EDTYPE;
+  if (!tokens || !target || !u || !path || !n_path || !next) return SELKV_EINVAL;
+  if (!aligned(target, 16) || !aligned(draft, 16) || !aligned(tokens, 4) || !aligned(parent, 4) || !aligned(u, 4) ||
+      !aligned(counts, 4) || !aligned(path, 4) || !aligned(n_path, 4) || !aligned(next, 4))
+    return SELKV_EALIGN;
+  if ((st = check_ws(ws, ws_bytes, tree_verify_bytes(batch, n, vocab))) != SELKV_OK) return st;
+  return hip_status(launch_tree_verify(batch, n, vocab, dtype, tokens, parent, target, draft, u, counts, path, n_path,
+                                       next, ws, stream));
+}
+
+SELKV_API selkv_status selkv_paged_keep(const selkv_params* p, const selkv_paged* c, const int32_t* path,
+                                        const int32_t* n_path, int32_t n, int32_t cache_len, const int32_t* lens,
+                                        hipStream_t stream) {
+  selkv_status st = check_paged(p, c, true);
+  if (st != SELKV_OK) return st;
+  if (n > kMaxNodes) return SELKV_EUNSUPPORTED;
+  if ((st = check_seqs(c, n, cache_len, !lens, lens, nullptr)) != SELKV_OK) return st;
+  if (!path || !n_path) return SELKV_EINVAL;
+  if (!aligned(path, 4) || !aligned(n_path, 4)) return SELKV_EALIGN;
+  return hip_status(launch_paged_keep(p->batch, p->n_heads_kv, p->head_dim, p->kv_dtype, view_paged(c),
+                                      Seqs{cache_len, n, lens, nullptr}, path, n_path, stream));
 }
 
 SELKV_API const char* selkv_status_string(selkv_status s) {

@@ -9,6 +9,7 @@ built library is missing -- there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -30,6 +31,9 @@ ROUTE_MODES = {"bucket": ROUTE_BUCKET, "full_cosine": ROUTE_FULL_COSINE, "bucket
 SELECT_MODES = {"per_head": SELECT_PER_HEAD, "union": SELECT_UNION}
 CODE_I8, CODE_E4M3 = 0, 1
 CODES8 = {"int8": CODE_I8, "e4m3": CODE_E4M3}
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_LAYOUTS = {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}
+MAX_NODES = 64
 
 
 class SelkvError(RuntimeError):
@@ -79,6 +83,41 @@ class Cache8Struct(ctypes.Structure):
     ]
 
 
+class PagedStruct(ctypes.Structure):
+    """selkv_paged."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("page", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+        ("columns", ctypes.c_int32),
+        ("K", ctypes.c_void_p),
+        ("V", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+    ]
+
+
+class RowsStruct(ctypes.Structure):
+    """selkv_rows."""
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("stride_b", ctypes.c_int64),
+        ("stride_n", ctypes.c_int64),
+        ("stride_h", ctypes.c_int64),
+    ]
+
+
+class RopeStruct(ctypes.Structure):
+    """selkv_rope."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("layout", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("freq", ctypes.c_void_p),
+    ]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run paper_2607_16213_amd.build.build() first")
@@ -86,6 +125,7 @@ def _load():
     vp, sz, i32, fp, ip = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p
     P = ctypes.POINTER(Params)
     C8 = ctypes.POINTER(Cache8Struct)
+    PG, RW, RP = ctypes.POINTER(PagedStruct), ctypes.POINTER(RowsStruct), ctypes.POINTER(RopeStruct)
     sigs = {
         "selkv_params_init": (None, [P]),
         "selkv_budget": (ctypes.c_int, [P, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32)]),
@@ -106,6 +146,14 @@ def _load():
         "selkv_decode8_workspace_size": (ctypes.c_int, [P, C8, ctypes.POINTER(sz)]),
         "selkv_decode8_attn": (ctypes.c_int, [P, C8, vp, fp, i32, ip, fp, vp, sz, vp]),
         "selkv_decode8_append": (ctypes.c_int, [P, C8, vp, vp, vp, fp, i32, ip, fp, vp, sz, vp]),
+        "selkv_paged_init": (None, [PG]),
+        "selkv_rope_init": (None, [RP]),
+        "selkv_paged_append": (ctypes.c_int, [P, PG, RW, RW, fp, RP, ip, RW, vp, i32, i32, ip, ip, vp]),
+        "selkv_tree_workspace_size": (ctypes.c_int, [P, PG, i32, ctypes.POINTER(sz)]),
+        "selkv_tree_attn": (ctypes.c_int, [P, PG, vp, ip, i32, i32, ip, ip, vp, vp, sz, vp]),
+        "selkv_tree_verify_workspace_size": (ctypes.c_int, [i32, i32, i32, ctypes.POINTER(sz)]),
+        "selkv_tree_verify": (ctypes.c_int, [i32, i32, i32, i32, ip, ip, vp, vp, fp, ip, ip, ip, ip, vp, sz, vp]),
+        "selkv_paged_keep": (ctypes.c_int, [P, PG, ip, ip, i32, i32, ip, vp]),
         "selkv_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "selkv_abi_version": (ctypes.c_int32, []),
     }
@@ -447,7 +495,7 @@ class Cache8:
         self.c.k_tail, self.c.v_tail = k_tail.data_ptr(), v_tail.data_ptr()
 
 
-def _check_cache8(p, cache, tensors, lens, counts, stream):
+def _check_cache(p, cache, tensors, lens, counts, stream):
     """Checks the cache against p and the current device, and (tensor, shape, dtype, name) of every tensor; returns the
     stream's handle.  The launch goes to the current device, so all of them have to be there."""
     if cache._of != (p.batch, p.n_heads_kv, p.head_dim, p.kv_dtype):
@@ -474,7 +522,7 @@ def cache8_write(p, cache, K_new, V_new, cache_len, lens=None, counts=None, stre
         raise ValueError("K_new must have four dimensions")
     n_new = K_new.shape[2]
     new, dt = (p.batch, p.n_heads_kv, n_new, p.head_dim), _kvdt(p)
-    on = _check_cache8(p, cache, ((K_new, new, dt, "K_new"), (V_new, new, dt, "V_new")), lens, counts, stream)
+    on = _check_cache(p, cache, ((K_new, new, dt, "K_new"), (V_new, new, dt, "V_new")), lens, counts, stream)
     if n_new == 0:
         return
     st = lib.selkv_cache8_write(p, cache.c, K_new.data_ptr(), V_new.data_ptr(), n_new, int(cache_len), _ptr(lens),
@@ -490,7 +538,7 @@ def cache8_read(p, cache, K_out, V_out, cache_len, first=0, lens=None, stream=No
         raise ValueError("K_out must have four dimensions")
     count = K_out.shape[2]
     out, dt = (p.batch, p.n_heads_kv, count, p.head_dim), _kvdt(p)
-    on = _check_cache8(p, cache, ((K_out, out, dt, "K_out"), (V_out, out, dt, "V_out")), lens, None, stream)
+    on = _check_cache(p, cache, ((K_out, out, dt, "K_out"), (V_out, out, dt, "V_out")), lens, None, stream)
     if count == 0:
         return
     st = lib.selkv_cache8_read(p, cache.c, K_out.data_ptr(), V_out.data_ptr(), int(first), count, int(cache_len),
@@ -519,7 +567,7 @@ def decode8_attn(p, cache, q, bias_in, cache_len, out, ws, lens=None, stream=Non
         raise ValueError(f"the workspace is on {ws.device}, the cache on {cache.device}")
     if bias_in is not None:
         ts += ((bias_in, (B, H, cache.capacity), _F32, "bias"),)
-    on = _check_cache8(p, cache, ts, lens, None, stream)
+    on = _check_cache(p, cache, ts, lens, None, stream)
     st = lib.selkv_decode8_attn(p, cache.c, q.data_ptr(), _ptr(bias_in), int(cache_len), _ptr(lens), out.data_ptr(),
                                 _ptr(ws), _nbytes(ws), on)
     if st:
@@ -536,11 +584,241 @@ def decode8_append(p, cache, q, k_new, v_new, bias_io, cache_len, out, ws, lens=
         raise ValueError(f"the workspace is on {ws.device}, the cache on {cache.device}")
     if bias_io is not None:
         ts += ((bias_io, (B, H, cache.capacity), _F32, "bias"),)
-    on = _check_cache8(p, cache, ts, lens, None, stream)
+    on = _check_cache(p, cache, ts, lens, None, stream)
     st = lib.selkv_decode8_append(p, cache.c, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _ptr(bias_io),
                                   int(cache_len), _ptr(lens), out.data_ptr(), _ptr(ws), _nbytes(ws), on)
     if st:
         raise SelkvError(st, "selkv_decode8_append")
+
+
+class PagedCache:
+    """A KV cache in pages of a pool: its buffers and the selkv_paged that names them.
+
+    `n_pages` pages of `page` entries, and a table of `columns` pages for every sequence, all -1 (no page) at first:
+    which page belongs to whom is the caller's to write into `table`, as the lengths are the caller's.  `over` takes
+    existing buffers."""
+
+    def __init__(self, p: Params, n_pages: int, columns: int, device, page: int = 64, bias: bool = True):
+        if page not in (16, 32, 64, 128, 256):
+            raise ValueError("page must be 16, 32, 64, 128 or 256")
+        B, H, d, dt = p.batch, p.n_heads_kv, p.head_dim, _kvdt(p)
+        zeros = lambda *shape, t: torch.zeros(shape, dtype=t, device=device)
+        self._take(p, zeros(n_pages, H, page, d, t=dt), zeros(n_pages, H, page, d, t=dt),
+                   torch.full((B, columns), -1, dtype=_I32, device=device),
+                   zeros(n_pages, H, page, t=_F32) if bias else None)
+
+    @classmethod
+    def over(cls, p: Params, K, V, table, bias=None) -> "PagedCache":
+        """A cache in buffers that the caller owns (the layouts of include/selkv.h): pages are those of K, columns
+        those of table."""
+        c = cls.__new__(cls)
+        c._take(p, K, V, table, bias)
+        return c
+
+    def _take(self, p, K, V, table, bias):
+        B, H, d, dt = p.batch, p.n_heads_kv, p.head_dim, _kvdt(p)
+        if K.dim() != 4 or table.dim() != 2:
+            raise ValueError("K must have four dimensions and table two")
+        n_pages, page, columns = K.shape[0], K.shape[2], table.shape[1]
+        if page not in (16, 32, 64, 128, 256) or n_pages < 1 or columns < 1:
+            raise ValueError(f"{n_pages} pages of {page} entries, {columns} columns: there must be some, of 16, 32, 64, "
+                             "128 or 256 entries")
+        pool = (n_pages, H, page, d)
+        _dev(K, pool, dt, "K"); _dev(V, pool, dt, "V"); _dev(table, (B, columns), _I32, "table")
+        if bias is not None:
+            _dev(bias, pool[:3], _F32, "bias")
+        if any(t is not None and t.device != K.device for t in (V, table, bias)):
+            raise ValueError("the buffers of a cache must be on one device")
+        self.K, self.V, self.table, self.bias, self.device = K, V, table, bias, K.device
+        self.page, self.n_pages, self.columns, self.capacity = page, n_pages, columns, columns * page
+        self._of = (B, H, d, p.kv_dtype)
+        self.c = PagedStruct()
+        lib.selkv_paged_init(self.c)
+        self.c.page, self.c.n_pages, self.c.columns = page, n_pages, columns
+        self.c.K, self.c.V, self.c.bias, self.c.table = K.data_ptr(), V.data_ptr(), _ptr(bias), table.data_ptr()
+
+
+def rope_frequencies(rot_dim: int, theta: float, device, scaling: str | None = None, factor: float = 1.0,
+                     original_len: int | None = None, fast: float = 32.0, slow: float = 1.0):
+    """(freq, scale) of a Rope: radians per position of the rot_dim / 2 pairs, theta^(-2 j / rot_dim) in float64 on
+    `device`, and what the rotated part is multiplied by.  For contexts `factor` times as long as those trained on:
+    "linear" divides every frequency by it; "ntk" stretches theta so that the lowest one is divided by it and the
+    highest stays; "yarn" (arXiv 2309.00071) divides those that turn less than `slow` times within original_len, keeps
+    those that turn more than `fast` times, goes linearly in j between, and multiplies by 0.1 ln(factor) + 1."""
+    if rot_dim < 2 or rot_dim % 2 or not theta > 1.0 or not factor >= 1.0:
+        raise ValueError("rot_dim must be even, theta above 1 and factor 1 or more")
+    j = torch.arange(rot_dim // 2, dtype=torch.float64)
+    scale = 1.0
+    if scaling == "ntk":
+        theta = theta * factor ** (rot_dim / (rot_dim - 2)) if rot_dim > 2 else theta
+    freq = theta ** (-2.0 * j / rot_dim)
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "yarn":
+        if not original_len or not fast > slow > 0:
+            raise ValueError("yarn needs original_len and fast > slow > 0")
+        # the pair that turns r times within original_len
+        pair = lambda r: rot_dim * math.log(original_len / (r * 2 * math.pi)) / (2 * math.log(theta))
+        lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), rot_dim - 1)
+        slowed = ((j - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
+        freq = freq * (1.0 - slowed) + freq / factor * slowed
+        scale = 0.1 * math.log(factor) + 1.0
+    elif scaling not in (None, "ntk"):
+        raise ValueError(f"scaling must be None, 'linear', 'ntk' or 'yarn', not {scaling!r}")
+    return freq.to(device), scale
+
+
+class Rope:
+    """Rotary positions of selkv_paged_append: freq [rot_dim / 2] float64 on the device, radians per position of each
+    pair; layout "half" pairs channel j with j + rot_dim / 2, "interleaved" 2 j with 2 j + 1; the rotated part is
+    multiplied by scale.  rot_dim is a multiple of 16 up to head_dim."""
+
+    def __init__(self, freq, layout: str = "half", scale: float = 1.0):
+        if freq.dim() != 1:
+            raise ValueError("freq must have one dimension")
+        _dev(freq, None, torch.float64, "freq")
+        self.freq, self.device = freq, freq.device
+        self.r = RopeStruct()
+        lib.selkv_rope_init(self.r)
+        self.r.layout, self.r.rot_dim, self.r.scale = ROPE_LAYOUTS[layout], 2 * freq.shape[0], float(scale)
+        self.r.freq = freq.data_ptr()
+
+
+def _rows(t, shape, dtype, name):
+    """selkv_rows of t [B, n, heads, d], whose rows are d elements side by side."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)} and dtype {t.dtype}, expected {tuple(shape)} and {dtype}")
+    s = t.stride()
+    if s[3] != 1:
+        raise ValueError(f"the channels of {name} must be contiguous")
+    if any(t.shape[i] > 1 and s[i] * t.element_size() % 16 for i in range(3)):
+        raise ValueError(f"the rows of {name} must be whole multiples of 16 bytes apart")
+    return RowsStruct(t.data_ptr(), *(s[i] if t.shape[i] > 1 else 0 for i in range(3)))
+
+
+def paged_append(p, cache, k_new, v_new, cache_len, lens=None, counts=None, bias_new=None, rope=None, positions=None,
+                 q=None, q_out=None, stream=None):
+    """Store rows k_new, v_new [B, n, H, d] (any strides, channels contiguous) behind the cache_len (or lens[b]) entries
+    of every sequence; counts [B] says how many of them each sequence gets.  With `rope`, keys are turned by positions
+    [B, n] (cache_len + i without them) on the way, and q [B, n, H G, d] into q_out.  bias_new [B, H, n] are the new
+    entries' biases, 0 without it."""
+    if k_new.dim() != 4:
+        raise ValueError("k_new must have four dimensions")
+    B, H, d, n, dt = p.batch, p.n_heads_kv, p.head_dim, k_new.shape[1], _kvdt(p)
+    k, v = _rows(k_new, (B, n, H, d), dt, "k_new"), _rows(v_new, (B, n, H, d), dt, "v_new")
+    on = [k_new, v_new]
+    ts = ()
+    if bias_new is not None:
+        ts += ((bias_new, (B, H, n), _F32, "bias_new"),)
+    if positions is not None:
+        ts += ((positions, (B, n), _I32, "positions"),)
+    qr = None
+    if q is not None:
+        if rope is None or q_out is None:
+            raise ValueError("q needs rope and q_out")
+        heads = (B, n, H * p.group, d)
+        qr = _rows(q, heads, dt, "q")
+        on.append(q)
+        ts += ((q_out, heads, dt, "q_out"),)
+    if rope is not None:
+        on.append(rope)
+    if any(t.device != cache.device for t in on):
+        raise ValueError(f"the rows and frequencies must be on {cache.device}, as the cache is")
+    st = _check_cache(p, cache, ts, lens, counts, stream)
+    if n == 0:
+        return
+    err = lib.selkv_paged_append(p, cache.c, k, v, _ptr(bias_new), None if rope is None else rope.r, _ptr(positions), qr,
+                                 None if q is None else q_out.data_ptr(), n, int(cache_len), _ptr(lens), _ptr(counts),
+                                 st)
+    if err:
+        raise SelkvError(err, "selkv_paged_append")
+
+
+def tree_workspace_bytes(p: Params, cache: PagedCache, n: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib.selkv_tree_workspace_size(p, cache.c, n, ctypes.byref(b)), "selkv_tree_workspace_size")
+    return b.value
+
+
+def tree_workspace(p: Params, cache: PagedCache, n: int) -> torch.Tensor:
+    """Scratch for tree_attn of up to n nodes at every length up to the capacity (needs no initialisation)."""
+    return torch.zeros(max(tree_workspace_bytes(p, cache, n), 1), dtype=torch.uint8, device=cache.device)
+
+
+def tree_attn(p, cache, q, parent, cache_len, out, ws, lens=None, counts=None, stream=None):
+    """Attention of the nodes q [B, n, H G, d] of a tree (parent [B, n], None for a chain) over the cache_len (or lens[b])
+    entries of every sequence and the nodes above, whose rows are the entries behind those; out as q."""
+    if q.dim() != 4:
+        raise ValueError("q must have four dimensions")
+    n = q.shape[1]
+    heads, dt = (p.batch, n, p.n_heads_kv * p.group, p.head_dim), _kvdt(p)
+    ts = ((q, heads, dt, "q"), (out, heads, dt, "out"))
+    if parent is not None:
+        ts += ((parent, (p.batch, n), _I32, "parent"),)
+    if ws is not None and ws.device != cache.device:
+        raise ValueError(f"the workspace is on {ws.device}, the cache on {cache.device}")
+    on = _check_cache(p, cache, ts, lens, counts, stream)
+    st = lib.selkv_tree_attn(p, cache.c, q.data_ptr(), _ptr(parent), n, int(cache_len), _ptr(lens), _ptr(counts),
+                             out.data_ptr(), _ptr(ws), _nbytes(ws), on)
+    if st:
+        raise SelkvError(st, "selkv_tree_attn")
+
+
+def tree_verify_workspace(batch: int, n: int, vocab: int, device) -> torch.Tensor:
+    """Scratch for tree_verify (needs no initialisation)."""
+    b = ctypes.c_size_t()
+    _check(lib.selkv_tree_verify_workspace_size(batch, n, vocab, ctypes.byref(b)), "selkv_tree_verify_workspace_size")
+    return torch.zeros(max(b.value, 1), dtype=torch.uint8, device=device)
+
+
+def tree_verify(tokens, parent, target, draft, u, path, n_path, next_token, ws, counts=None, stream=None):
+    """Accept a path of every tree and draw the token after it.  tokens, parent (None: a chain), path [B, n] int32;
+    target and draft (None: drafted without a distribution) [B, n, vocab], fp32 or bf16: node i's row is the
+    distribution after it; u [B, n] fp32 in [0, 1), u[:, i] for node i and u[:, 0] for the last token; n_path,
+    next_token, counts [B] int32."""
+    if target.dim() != 3:
+        raise ValueError("target must have three dimensions")
+    if target.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"target has dtype {target.dtype}, expected torch.float32 or torch.bfloat16")
+    B, n, vocab = target.shape
+    dev = target.device
+    ts = [(target, (B, n, vocab), target.dtype, "target"), (tokens, (B, n), _I32, "tokens"), (u, (B, n), _F32, "u"),
+          (path, (B, n), _I32, "path"), (n_path, (B,), _I32, "n_path"), (next_token, (B,), _I32, "next_token")]
+    if parent is not None:
+        ts.append((parent, (B, n), _I32, "parent"))
+    if draft is not None:
+        ts.append((draft, (B, n, vocab), target.dtype, "draft"))
+    if counts is not None:
+        ts.append((counts, (B,), _I32, "counts"))
+    for t, shape, dtype, name in ts:
+        _dev(t, shape, dtype, name)
+        if t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, target on {dev}")
+    if ws is not None and ws.device != dev:
+        raise ValueError(f"the workspace is on {ws.device}, target on {dev}")
+    if dev.index != torch.cuda.current_device() or (stream is not None and stream.device != dev):
+        raise ValueError(f"target is on {dev}: it must be the current device, and that of the stream")
+    st = lib.selkv_tree_verify(B, n, vocab, BF16 if target.dtype == torch.bfloat16 else F32, tokens.data_ptr(),
+                               _ptr(parent), target.data_ptr(), _ptr(draft), u.data_ptr(), _ptr(counts),
+                               path.data_ptr(), n_path.data_ptr(), next_token.data_ptr(), _ptr(ws), _nbytes(ws),
+                               _stream(stream))
+    if st:
+        raise SelkvError(st, "selkv_tree_verify")
+
+
+def paged_keep(p, cache, path, n_path, cache_len, lens=None, stream=None):
+    """Move the rows of the nodes path[b, :n_path[b]] to the front of their tree's, entries cache_len (or lens[b]) on.
+    lens is read only: advance it by n_path after the call."""
+    if path.dim() != 2:
+        raise ValueError("path must have two dimensions")
+    n = path.shape[1]
+    on = _check_cache(p, cache, ((path, (p.batch, n), _I32, "path"), (n_path, (p.batch,), _I32, "n_path")), lens, None,
+                       stream)
+    st = lib.selkv_paged_keep(p, cache.c, path.data_ptr(), n_path.data_ptr(), n, int(cache_len), _ptr(lens), on)
+    if st:
+        raise SelkvError(st, "selkv_paged_keep")
 
 
 class Compressor:
@@ -598,6 +876,14 @@ class Compressor:
                 bias_out[:, :, :self.m].copy_(self.bias)
         return cache
 
+    def store_paged(self, cache: PagedCache, stream=None):
+        """Append the compressed cache of the last run, and its biases where the cache has them, to the empty sequences
+        of a paged cache (each then holds m entries).  Its keys carry their positions already."""
+        rows = lambda x: x.transpose(1, 2)
+        paged_append(self.p, cache, rows(self.K_out), rows(self.V_out), 0,
+                     bias_new=None if cache.bias is None else self.bias, stream=stream)
+        return cache
+
     def outputs(self):
         return dict(score=self.score, attn=self.attn, vnorm=self.vnorm, kept=self.kept, evicted=self.evicted,
                     K_out=self.K_out, V_out=self.V_out, target=self.target, gate=self.gate, bias=self.bias)
@@ -638,3 +924,43 @@ class Decoder8:
         o = self.out if out is None else out
         decode8_append(self.p, self.cache, q, k_new, v_new, bias_io, cache_len, o, self.ws, lens, stream)
         return o
+
+
+class TreeDecoder:
+    """Owns the buffers of generation steps with trees of up to n nodes over one paged cache: attend, verify (where
+    `vocab` is given) and keep, in this order.  A step of fewer nodes uses the front of them."""
+
+    def __init__(self, p: Params, cache: PagedCache, n: int, vocab: int | None = None):
+        self.p, self.cache, self.n, self.vocab = p, cache, n, vocab
+        dev, heads = cache.device, p.n_heads_kv * p.group
+        self.ws = tree_workspace(p, cache, n)
+        self.out, self.q = (torch.zeros((p.batch, n, heads, p.head_dim), dtype=_kvdt(p), device=dev) for _ in range(2))
+        self.path = torch.zeros((p.batch, n), dtype=_I32, device=dev)
+        self.n_path, self.next_token = (torch.zeros((p.batch,), dtype=_I32, device=dev) for _ in range(2))
+        self.ws_verify = tree_verify_workspace(p.batch, n, vocab, dev) if vocab else None
+
+    def _front(self, t, n):
+        if n > self.n:
+            raise ValueError(f"{n} nodes, made for {self.n}")
+        return t.view(-1)[:t.numel() // self.n * n].view(t.shape[0], n, *t.shape[2:])
+
+    def attend(self, q, k_new, v_new, cache_len, parent=None, lens=None, counts=None, rope=None, positions=None,
+               stream=None):
+        """Append the nodes' rows k_new, v_new [B, n, H, d] and attend with q [B, n, H G, d]; where rope is given, q and
+        k_new are turned by positions [B, n] (cache_len + i without them) first."""
+        out = self._front(self.out, q.shape[1])
+        turned = None if rope is None else self._front(self.q, q.shape[1])
+        paged_append(self.p, self.cache, k_new, v_new, cache_len, lens, counts, rope=rope, positions=positions,
+                     q=None if rope is None else q, q_out=turned, stream=stream)
+        tree_attn(self.p, self.cache, q if rope is None else turned, parent, cache_len, out, self.ws, lens, counts, stream)
+        return out
+
+    def verify(self, tokens, target, draft, u, parent=None, counts=None, stream=None):
+        """(path, n_path, next_token) of selkv_tree_verify."""
+        path = self._front(self.path, tokens.shape[1])
+        tree_verify(tokens, parent, target, draft, u, path, self.n_path, self.next_token, self.ws_verify, counts, stream)
+        return path, self.n_path, self.next_token
+
+    def keep(self, path, n_path, cache_len, lens=None, stream=None):
+        """Keep the rows of the path; the caller advances its lengths by n_path."""
+        paged_keep(self.p, self.cache, path, n_path, cache_len, lens, stream)
