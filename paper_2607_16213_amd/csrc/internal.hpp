@@ -182,13 +182,16 @@ struct RowsIn {
 
 struct TreePlan {
   int row_tiles;       // 16-row tiles of a wave
-  bool split_rows;     // the waves of a workgroup take rows of their own, otherwise entries of their own
+  int row_groups;      // groups of a workgroup's waves that take rows of their own; within one they share rows
+  int key_groups;      // waves of a group, which take entries in turn
   int row_blocks;      // workgroups that share a KV head's entries
+  int step;            // entries that the waves of a workgroup take at a time: splits are whole multiples
   int splits;          // workgroups along the entries
   size_t ml_off, bytes;
 };
 
-TreePlan plan_tree(int64_t heads, int entries, int d, int rows, size_t elem);   // entries: the most a sequence can have
+// entries: the most a sequence can have; ragged: their lengths are on the device
+TreePlan plan_tree(int64_t heads, int entries, int d, int rows, size_t elem, bool ragged);
 size_t tree_workspace_bound(int64_t heads, int capacity, int d, int G, int n, size_t elem);
 
 hipError_t launch_paged_append(int batch, int hkv, int d, int dtype, const Paged& c, const Seqs& n, const RowsIn& k,

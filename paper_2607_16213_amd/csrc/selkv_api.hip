@@ -689,7 +689,7 @@ SELKV_API selkv_status selkv_tree_attn(const selkv_params* p, const selkv_paged*
   const int32_t capacity = c->columns * c->page;
   const int32_t entries = n > capacity - cache_len ? capacity : cache_len + n;
   const TreePlan plan =
-      plan_tree((int64_t)p->batch * p->n_heads_kv, entries, p->head_dim, n * p->group, elem_size(p));
+      plan_tree((int64_t)p->batch * p->n_heads_kv, entries, p->head_dim, n * p->group, elem_size(p), lens != nullptr);
   if ((st = check_ws(ws, ws_bytes, plan.bytes)) != SELKV_OK) return st;
   return hip_status(launch_tree_attn(p->batch, p->n_heads_kv, p->head_dim, p->group, p->kv_dtype, eff_scale(p), plan,
                                      view_paged(c), Seqs{cache_len, n, lens, counts}, q, parent, out, ws, stream));

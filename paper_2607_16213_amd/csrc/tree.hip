@@ -35,12 +35,14 @@
 namespace selkv {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * 64;
 constexpr int kTile = 32;              // entries of a wave's step
-constexpr int kStep = kWaves * kTile;  // splits are whole multiples of it
-constexpr int kTargetBlocks = 768;
+constexpr int kCUs = 256;
 constexpr int kMaxSplit = 256;
+constexpr int kMaxRounds = 4;          // of workgroups, one a CU
+constexpr int kRaggedRounds = 3;
+constexpr int kGroupCost = 160;        // of a workgroup, and of the second kernel, in entries
+constexpr int kCombineCost = 256;
+constexpr int kFewSlots = 8;           // up to which a row is combined by d/4 threads
 
 struct TreeArgs {
   Paged c;
@@ -50,14 +52,18 @@ struct TreeArgs {
   char* out;
   float* part_o;     // [B hkv, splits, n G, D]
   float2* part_ml;   // [B hkv, splits, n G]
-  int hkv, G, splits, row_blocks;
+  int hkv, G, splits, row_blocks, step;
   float scale;
 };
 
+// Tiles of 32 entries that a wave of a shared tile takes one after the other: with two there are half as many barriers
+// (64 nodes over 25600 entries 78.4 us, 80.4 with one).
+constexpr int tiles_of_turn(int key_groups) { return key_groups == 1 ? 2 : 1; }
+
 // Entries of a split of a sequence of `total`: as many splits as there are, of whole steps.
-__device__ __forceinline__ int chunk_of(int splits, int total) {
-  const uint32_t per = ((uint32_t)total + splits - 1) / (uint32_t)splits;
-  return (int)(max((per + kStep - 1) / kStep, 1u) * kStep);
+__device__ __forceinline__ int chunk_of(const TreeArgs& a, int total) {
+  const uint32_t per = ((uint32_t)total + a.splits - 1) / (uint32_t)a.splits, step = a.step;
+  return (int)(max((per + step - 1) / step, 1u) * step);
 }
 
 __device__ __forceinline__ float weight_of(float m, float M) { return m == kNegInf ? 0.f : fast_exp2((m - M) * kLog2e); }
@@ -97,53 +103,132 @@ __device__ __forceinline__ uint64_t ancestors(const int32_t* parent, int n, int 
   return seen;
 }
 
-// What a wave reads for 32 entries.
+// The table's columns from `first` on, one in each lane of the wave.
+struct PageWindow {
+  int first, page;
+  // `whole`: where entries end that are to be read without a check; moved to the first of them that is on no page
+  __device__ __forceinline__ void fill(const Paged& c, uint32_t b, int column, int& whole, int lane) {
+    first = column;
+    page = c.table[(size_t)b * c.columns + min(column + lane, c.columns - 1)];
+    const uint64_t none = __ballot((uint32_t)page >= (uint32_t)c.n_pages || column + lane >= c.columns);
+    if (none) whole = min(whole, (column + __ffsll((unsigned long long)none) - 1) << c.shift);
+  }
+  __device__ __forceinline__ bool holds(const Paged& c, int entry) const { return (entry >> c.shift) < first + 64; }
+  __device__ __forceinline__ int at(const Paged& c, int entry) const {
+    return __shfl(page, (entry >> c.shift) - first, 64);
+  }
+};
+
+// What a wave reads for 32 entries: 16-byte chunks of the K rows of its two tiles and the biases of entries 8 grp .. + 7,
+// and its words of the V rows of these.
 template <typename T, int D>
-struct Entries {
-  static constexpr int KC = D * (int)sizeof(T) / 64;       // 16-byte chunks of a lane of a K tile row
-  static constexpr int VW = D * (int)sizeof(T) / 64;       // words of a lane of a V row
-  Chunk16 k[2][KC];
-  uint32_t v[8][VW];
-  float bias[8];                                           // of entries 8 grp .. + 7
+struct Keys {
+  static constexpr int N = D * (int)sizeof(T) / 64;
+  Chunk16 k[2][N];
+  float bias[8];
+  __device__ __forceinline__ void load(const Paged& c, int hkv, int head, int base, int pk, int pv, int col, int grp) {
+    constexpr int RB = D * (int)sizeof(T);
+    const char* kp = c.K + row_of(c, hkv, pk, head, base + 8 * (col >> 2) + (col & 3)) * RB + grp * 16;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < N; ++j) k[t][j] = load16(kp + 4 * t * RB + j * 64);
+    // without biases the pool of K is read in their place (it is larger) and passed over: no branch between the loads
+    const float* bp =
+        (c.bias ? c.bias : reinterpret_cast<const float*>(c.K)) + row_of(c, hkv, pv, head, base + 8 * grp);
+    const Chunk16 b0 = load16(bp), b1 = load16(bp + 4);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      bias[s] = __uint_as_float(b0.w[s]);
+      bias[4 + s] = __uint_as_float(b1.w[s]);
+    }
+  }
 };
 
 template <typename T, int D>
-__device__ __forceinline__ void load_entries(Entries<T, D>& x, const Paged& c, int hkv, int head, int base, int pk,
-                                             int pv, int col, int grp) {
+struct Values {
+  static constexpr int N = D * (int)sizeof(T) / 64;
+  uint32_t v[8][N];
+  __device__ __forceinline__ void load(const Paged& c, int hkv, int head, int base, int pv, int col, int grp) {
+    constexpr int RB = D * (int)sizeof(T);
+    const char* vp = c.V + row_of(c, hkv, pv, head, base + 8 * grp) * RB + col * (RB / 16);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      if constexpr (RB / 16 >= 16) {
+#pragma unroll
+        for (int i = 0; i < RB / 256; ++i) {
+          const Chunk16 w = load16(vp + s * RB + i * 16);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[s][4 * i + k] = w.w[k];
+        }
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(vp + s * RB);
+        v[s][0] = w.x;
+        v[s][1] = w.y;
+      }
+    }
+  }
+};
+
+// The same from a tile in LDS.  Rows are RB bytes one after the other; 16-byte chunk c of row r is at chunk c ^ swizzle(r),
+// so that the eight rows whose chunks c are read together, 8 a + b with a = 0, 1 and b = 0 .. 3 (or 4 .. 7), are on
+// different banks.
+__device__ __forceinline__ int swizzle(int row) { return (row & 3) | ((row >> 1) & 4); }
+
+// The places of a lane's chunks: only bit 2 of the swizzle meets bits of j and bits 0 and 1 those of s, so few are kept.
+template <typename T, int D>
+struct Places {
+  static constexpr int RB = D * (int)sizeof(T);
+  static constexpr int VC = RB / 16 >= 16 ? RB / 256 : 1;   // 16-byte chunks (or half of one) of a lane of a V row
+  int k[2], v[4][VC], bias;
+  __device__ __forceinline__ Places(int col, int grp) {
+    const int row = 8 * (col >> 2) + (col & 3);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) k[j] = row * RB + (((4 * j + grp) ^ swizzle(row)) << 4);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int i = 0; i < VC; ++i) {
+        const int chunk = RB / 16 >= 16 ? col * VC + i : col >> 1;
+        v[s][i] = (8 * grp + s) * RB + ((chunk ^ swizzle(8 * grp + s)) << 4) + (RB / 16 >= 16 ? 0 : (col & 1) * 8);
+      }
+    bias = 32 * grp;
+  }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void read_keys(Keys<T, D>& x, const char* tile, const char* bias, const Places<T, D>& at) {
   constexpr int RB = D * (int)sizeof(T);
-  const char* kp = c.K + row_of(c, hkv, max(pk, 0), head, base + 8 * (col >> 2) + (col & 3)) * RB + grp * 16;
-  const size_t vr = row_of(c, hkv, max(pv, 0), head, base + 8 * grp);
-  const char* vp = c.V + vr * RB + col * (RB / 16);
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int j = 0; j < Entries<T, D>::KC; ++j) x.k[t][j] = load16(kp + 4 * t * RB + j * 64);
+    for (int j = 0; j < Keys<T, D>::N; ++j) x.k[t][j] = load16(tile + at.k[j & 1] + (j >> 1) * 128 + 4 * t * RB);
+  const Chunk16 b0 = load16(bias + at.bias), b1 = load16(bias + at.bias + 16);
 #pragma unroll
-  for (int s = 0; s < 8; ++s) {
-    if constexpr (RB / 16 >= 16) {
+  for (int s = 0; s < 4; ++s) {
+    x.bias[s] = __uint_as_float(b0.w[s]);
+    x.bias[4 + s] = __uint_as_float(b1.w[s]);
+  }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void read_values(Values<T, D>& x, const char* tile, const Places<T, D>& at) {
+  constexpr int RB = D * (int)sizeof(T);
 #pragma unroll
-      for (int i = 0; i < RB / 256; ++i) {
-        const Chunk16 w = load16(vp + s * RB + i * 16);
+  for (int s = 0; s < 8; ++s)
+#pragma unroll
+    for (int i = 0; i < Places<T, D>::VC; ++i) {
+      const char* from = tile + at.v[s & 3][i] + (s >> 2) * 4 * RB;
+      if constexpr (RB / 16 >= 16) {
+        const Chunk16 w = load16(from);
 #pragma unroll
         for (int k = 0; k < 4; ++k) x.v[s][4 * i + k] = w.w[k];
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(from);
+        x.v[s][0] = w.x;
+        x.v[s][1] = w.y;
       }
-    } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(vp + s * RB);
-      x.v[s][0] = w.x;
-      x.v[s][1] = w.y;
     }
-  }
-  if (c.bias) {
-    const Chunk16 b0 = load16(c.bias + vr), b1 = load16(c.bias + vr + 4);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      x.bias[s] = __uint_as_float(b0.w[s]);
-      x.bias[4 + s] = __uint_as_float(b1.w[s]);
-    }
-  } else {
-#pragma unroll
-    for (int s = 0; s < 8; ++s) x.bias[s] = 0.f;
-  }
 }
 
 // Softmax state of a wave's row tile: lane (column, grp) keeps its row's maximum, the sum over the entries it holds,
@@ -167,7 +252,7 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t& hi, uint32_
 
 // O^T += V^T P^T for RT row tiles whose weights are p.
 template <typename T, int D, int RT>
-__device__ __forceinline__ void add_values(RowTile<D> (&st)[RT], const uint32_t (&v)[8][Entries<T, D>::VW],
+__device__ __forceinline__ void add_values(RowTile<D> (&st)[RT], const uint32_t (&v)[8][Values<T, D>::N],
                                            const float (&p)[RT][8]) {
   if constexpr (sizeof(T) == 2) {
     Chunk16 hi[RT], lo[RT];
@@ -234,64 +319,92 @@ __device__ __forceinline__ uint32_t zero_unbounded(uint32_t w, bool& any) {
 
 template <typename T, int D, int RT>
 struct Rows {
-  Chunk16 q[RT][Entries<T, D>::KC];
+  Chunk16 q[RT][Keys<T, D>::N];
   uint64_t seen[RT];   // the nodes that the row attends to
 };
 
-// One step: 32 entries from `base`.  len: entries that all rows attend to, end: with the nodes' behind them.
+// Logits of 32 entries, S = K Q^T scaled and biased.
 template <typename T, int D, int RT>
-__device__ __forceinline__ void attend(RowTile<D> (&st)[RT], Entries<T, D>& x, const Rows<T, D, RT>& rows,
-                                       const TreeArgs& a, uint32_t b, int head, int base, int len, int end, int pv,
-                                       bool careful, int grp) {
-  float p[RT][8];
+__device__ __forceinline__ void logits(float (&p)[RT][8], const Keys<T, D>& x, const Rows<T, D, RT>& rows, float scale,
+                                       bool has_bias) {
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < Entries<T, D>::KC; ++j) s = Mma<T>::step(x.k[h][j], rows.q[t][j], s);
+      for (int j = 0; j < Keys<T, D>::N; ++j) s = Mma<T>::step(x.k[h][j], rows.q[t][j], s);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) p[t][4 * h + r] = fmaf(s[r], a.scale, x.bias[4 * h + r]);
+      for (int r = 0; r < 4; ++r) p[t][4 * h + r] = fmaf(s[r], scale, has_bias ? x.bias[4 * h + r] : 0.f);
     }
-  const bool edge = careful || base + kTile > len || __any(pv < 0);
-  bool unbounded = false;
-  if (edge) {
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      const int entry = base + 8 * grp + s, node = entry - len;
-      const bool live = pv >= 0 && entry < end && x.bias[s] != kNegInf;
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-        if (!(live && (node < 0 || ((rows.seen[t] >> (node & 63)) & 1)))) p[t][s] = kNegInf;
-#pragma unroll
-      for (int w = 0; w < Entries<T, D>::VW; ++w) {
-        if (!live) x.v[s][w] = 0u;
-        else if (careful) x.v[s][w] = zero_unbounded<T>(x.v[s][w], unbounded);
-      }
-    }
-  }
+}
+
+// A row's maximum follows its logits only when they are this far above it, so that after the first tiles of a row hardly a
+// tile has to rescale what is there (one of 32 rows is enough for that: 172 us where 183 without, 16 sequences of 0 to
+// 8100 entries, 26 nodes).  Weights are up to e^6 then, which fp32 sums and the weights' relative rounding do not mind.
+constexpr float kSlack = 6.f;
+
+// Logits to weights, with the running maximum and sum.  Before bf16 weights the maximum is taken off by the fma that
+// turns a logit to powers of two (its product with log2(e), rounded once, is the same for all of a row); a maximum
+// beyond 2^127 / log2(e) makes that infinite, and the results NaN: a careful pass takes such a one off by itself.
+template <bool FUSED, int D, int RT>
+__device__ __forceinline__ void soften(RowTile<D> (&st)[RT], float (&p)[RT][8], bool careful) {
+  float top[RT];
+  bool above = false;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     float mx = p[t][0];
 #pragma unroll
     for (int s = 1; s < 8; ++s) mx = fmaxf(mx, p[t][s]);
-    mx = max_xor32(max_xor16(mx));
-    const float mnew = fmaxf(st[t].m, mx);
-    const float ref = mnew == kNegInf ? 0.f : mnew;   // nothing unmasked yet: every weight is 0
-    if (__any(mnew != st[t].m)) {
-      const float corr = fast_exp2((st[t].m - ref) * kLog2e);
+    top[t] = max_xor32(max_xor16(mx));
+    above = above || top[t] > st[t].m + kSlack;
+  }
+  if (__builtin_expect(__any(above), 0)) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float m = top[t] > st[t].m + kSlack ? top[t] : st[t].m;   // by row: none depends on the others
+      const float corr = m == st[t].m ? 1.f : weight_of(st[t].m, m);
       st[t].l *= corr;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) st[t].o[i] *= corr;
-      st[t].m = mnew;
+      st[t].m = m;
     }
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const float ref = st[t].m == kNegInf ? 0.f : st[t].m;   // nothing unmasked yet: every weight is 0
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      p[t][s] = fast_exp2((p[t][s] - ref) * kLog2e);
+      if (FUSED && !(careful && !finite(ref * kLog2e))) p[t][s] = fast_exp2(fmaf(p[t][s], kLog2e, -ref * kLog2e));
+      else p[t][s] = fast_exp2((p[t][s] - ref) * kLog2e);
       st[t].l += p[t][s];
     }
   }
+}
+
+// A step whose 32 entries from `base` may be behind len, the entries that all rows attend to, behind end, the nodes after
+// them, or on no page (pv < 0); or one of a careful pass.
+template <typename T, int D, int RT>
+__device__ __forceinline__ void attend_edge(RowTile<D> (&st)[RT], const Keys<T, D>& k, Values<T, D>& x,
+                                            const Rows<T, D, RT>& rows, const TreeArgs& a, uint32_t b, int head, int base,
+                                            int len, int end, int pv, bool careful, int grp) {
+  float p[RT][8];
+  logits<T, D, RT>(p, k, rows, a.scale, a.c.bias != nullptr);
+  bool unbounded = false;
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    const int entry = base + 8 * grp + s, node = entry - len;
+    const bool live = pv >= 0 && entry < end && !(a.c.bias && k.bias[s] == kNegInf);
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+      if (!(live && (node < 0 || ((rows.seen[t] >> (node & 63)) & 1)))) p[t][s] = kNegInf;
+#pragma unroll
+    for (int w = 0; w < Values<T, D>::N; ++w) {
+      if (!live) x.v[s][w] = 0u;
+      else if (careful) x.v[s][w] = zero_unbounded<T>(x.v[s][w], unbounded);
+    }
+  }
+  soften<sizeof(T) == 2, D, RT>(st, p, careful);
   add_values<T, D, RT>(st, x.v, p);
   if (careful && __any(unbounded)) {
     for (int s = 0; s < kTile; ++s) {
@@ -305,6 +418,21 @@ __device__ __forceinline__ void attend(RowTile<D> (&st)[RT], Entries<T, D>& x, c
       for (int t = 0; t < RT; ++t) seen[t] = node < 0 || ((rows.seen[t] >> (node & 63)) & 1);
       add_unbounded<T, D, RT>(st, a.c.V + row * D * sizeof(T), seen, grp);
     }
+  }
+}
+
+// Steps of a wave from e on, entries of any kind.
+template <typename T, int D, int RT>
+__device__ __forceinline__ void attend_edges(RowTile<D> (&st)[RT], const Rows<T, D, RT>& rows, const TreeArgs& a,
+                                             uint32_t b, int head, int e, int e1, int step, int len, int end,
+                                             bool careful, int col, int grp) {
+  for (; e < e1; e += step) {
+    const int pk = page_of(a.c, b, e + 8 * (col >> 2)), pv = page_of(a.c, b, e + 8 * grp);
+    Keys<T, D> k;
+    Values<T, D> v;
+    k.load(a.c, a.hkv, head, e, max(pk, 0), max(pv, 0), col, grp);
+    v.load(a.c, a.hkv, head, e, max(pv, 0), col, grp);
+    attend_edge<T, D, RT>(st, k, v, rows, a, b, head, e, len, end, pv, careful, grp);
   }
 }
 
@@ -328,91 +456,43 @@ __device__ __forceinline__ void store_row(char* row, const f32x4 (&o)[D / 16], i
   }
 }
 
-template <typename T, int D, int RT>
-__global__ __launch_bounds__(kThreads, 2) void tree_kernel(TreeArgs a) {
-  constexpr int ROWS = 16 * RT;
+// The end of a split: the results of the KG waves that share rows meet in LDS, two and two, and go to the outputs or the
+// workspace.  s_o: RG KG / 2 runs of RT d/16 x 64 slots, s_ml: of RT x 64.
+template <typename T, int D, int RT, int RG, int KG>
+__device__ __forceinline__ void finish(RowTile<D> (&st)[RT], f32x4* s_o, float2* s_ml, const TreeArgs& a, uint32_t b,
+                                       int head, int row0, int nrows, int split, int rw, int kw, int lane) {
   constexpr int RB = D * (int)sizeof(T);
-  __shared__ __align__(16) f32x4 s_o[2][RT * (D / 16)][64];
-  __shared__ float2 s_ml[2][RT][64];
-  const uint32_t bh = blockIdx.y, b = bh / (uint32_t)a.hkv;
-  const int head = bh - b * a.hkv;
-  const int split = blockIdx.x % a.splits, rb = blockIdx.x / a.splits;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
-  int len, count;
-  if (!sequence_of(a.n, b, len, count)) return;
-  const int nrows = count * a.G, row0 = rb * ROWS;
-  if (row0 >= nrows) return;
-  const int end = len + count;
-  const int chunk = chunk_of(a.splits, end);
-  const int e0 = split * chunk, e1 = min(e0 + chunk, end);
-  if (e0 >= e1) return;                  // behind a shorter sequence's end: the combining kernel does not read the slot
-
-  Rows<T, D, RT> rows;
-  const uint64_t anc = e1 > len ? ancestors(a.parent ? a.parent + (size_t)b * a.n.n : nullptr, a.n.n, lane) : 0;
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int r = row0 + 16 * t + col, node = r < nrows ? r / a.G : 0, g = r < nrows ? r - node * a.G : 0;
-    const char* qr = a.q + (((size_t)b * a.n.n + node) * a.hkv + head) * a.G * RB + (size_t)g * RB + grp * 16;
-#pragma unroll
-    for (int j = 0; j < Entries<T, D>::KC; ++j) rows.q[t][j] = load16(qr + j * 64);
-    rows.seen[t] = __shfl((unsigned long long)anc, node, 64);
-  }
-  RowTile<D> st[RT];
-  bool careful = false;
-  for (;;) {
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      st[t].m = kNegInf;
-      st[t].l = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) st[t].o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    for (int e = e0 + wave * kTile; e < e1; e += kStep) {
-      const int pk = page_of(a.c, b, e + 8 * (col >> 2)), pv = page_of(a.c, b, e + 8 * grp);
-      Entries<T, D> x;
-      load_entries<T, D>(x, a.c, a.hkv, head, e, pk, pv, col, grp);
-      attend<T, D, RT>(st, x, rows, a, b, head, e, len, end, pv, careful, grp);
-    }
-    bool fine = true;
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) fine = fine && finite(st[t].o[i][r]);
-    if (careful || !__any(!fine)) break;
-    careful = true;
-  }
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     st[t].l = add_xor32(add_xor16(st[t].l));
     st[t].m = nan_counts(st[t].m, st[t].l);
   }
-
-  // the waves' results, two and two
 #pragma unroll
-  for (int step = kWaves / 2; step > 0; step /= 2) {
-    if (wave >= step && wave < 2 * step) {
+  for (int step = KG / 2; step > 0; step /= 2) {
+    const int slot = rw * step + (kw >= step ? kw - step : kw);
+    f32x4* so = s_o + slot * RT * (D / 16) * 64 + lane;
+    float2* sm = s_ml + slot * RT * 64 + lane;
+    if (kw >= step && kw < 2 * step) {
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        s_ml[wave - step][t][lane] = make_float2(st[t].m, st[t].l);
+        sm[t * 64] = make_float2(st[t].m, st[t].l);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) s_o[wave - step][t * (D / 16) + i][lane] = st[t].o[i];
+        for (int i = 0; i < D / 16; ++i) so[(t * (D / 16) + i) * 64] = st[t].o[i];
       }
     }
     __syncthreads();
-    if (wave < step) {
+    if (kw < step) {
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        const float2 ml = s_ml[wave][t][lane];
+        const float2 ml = sm[t * 64];
         const float M = fmaxf(st[t].m, ml.x);
         const float c0 = weight_of(st[t].m, M), c1 = weight_of(ml.x, M);
         const bool some0 = st[t].m != kNegInf, some1 = ml.x != kNegInf;   // a part without entries has weight 0 and 0s
         st[t].l = (some0 ? st[t].l * c0 : 0.f) + (some1 ? ml.y * c1 : 0.f);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-          const f32x4 o = s_o[wave][t * (D / 16) + i][lane];
+          const f32x4 o = so[(t * (D / 16) + i) * 64];
 #pragma unroll
           for (int r = 0; r < 4; ++r) st[t].o[i][r] = (some0 ? st[t].o[i][r] * c0 : 0.f) + (some1 ? o[r] * c1 : 0.f);
         }
@@ -421,7 +501,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(TreeArgs a) {
     }
     __syncthreads();
   }
-  if (wave > 0) return;
+  if (kw > 0) return;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int r = row0 + 16 * t + col;
@@ -435,40 +515,324 @@ __global__ __launch_bounds__(kThreads, 2) void tree_kernel(TreeArgs a) {
         for (int k = 0; k < 4; ++k) o[i][k] = st[t].l == 0.f ? 0.f : st[t].o[i][k] / st[t].l;
       store_row<T, D>(a.out + ((((size_t)b * a.n.n + node) * a.hkv + head) * a.G + g) * RB, o, grp);
     } else {
-      const size_t part = ((size_t)bh * a.splits + split) * ((size_t)a.n.n * a.G) + r;
+      const size_t part = (((size_t)b * a.hkv + head) * a.splits + split) * ((size_t)a.n.n * a.G) + r;
       store_row<float, D>(reinterpret_cast<char*>(a.part_o + part * D), st[t].o, grp);
       if (grp == 0) a.part_ml[part] = make_float2(st[t].m, st[t].l);
     }
   }
 }
 
-// Combines the partials of a row, in order: d/4 threads with four channels each.
-template <typename T, int D>
+// Queries of a wave's rows and the nodes that they attend to (`anc`: ancestors() of the lane's node).
+template <typename T, int D, int RT>
+__device__ __forceinline__ void load_rows(Rows<T, D, RT>& rows, const TreeArgs& a, uint32_t b, int head, int row0,
+                                          int nrows, uint64_t anc, int col, int grp) {
+  constexpr int RB = D * (int)sizeof(T);
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int r = row0 + 16 * t + col, node = r < nrows ? r / a.G : 0, g = r < nrows ? r - node * a.G : 0;
+    const char* qr = a.q + (((size_t)b * a.n.n + node) * a.hkv + head) * a.G * RB + (size_t)g * RB + grp * 16;
+#pragma unroll
+    for (int j = 0; j < Keys<T, D>::N; ++j) rows.q[t][j] = load16(qr + j * 64);
+    rows.seen[t] = __shfl((unsigned long long)anc, node, 64);
+  }
+}
+
+template <int D, int RT>
+__device__ __forceinline__ void clear(RowTile<D> (&st)[RT]) {
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    st[t].m = kNegInf;
+    st[t].l = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) st[t].o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+
+template <int D, int RT>
+__device__ __forceinline__ bool all_finite(const RowTile<D> (&st)[RT]) {
+  bool fine = true;
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) fine = fine && finite(st[t].o[i][r]);
+  return fine;
+}
+
+// Waves a SIMD is to hold: what the registers of a row tile's accumulators and queries leave.
+template <typename T, int D, int RT>
+constexpr int waves_per_simd() {
+  return RT == 2 ? (sizeof(T) == 4 && D == 128 ? 1 : 2) : sizeof(T) == 4 && D == 128 ? 2 : 3;
+}
+
+// A workgroup is RG groups of waves with RT 16-row tiles of their own; the KG waves of a group share the rows and take
+// entries in turn.
+template <typename T, int D, int RT, int RG, int KG>
+__global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, RT>())) void tree_kernel(TreeArgs a) {
+  constexpr int ROWS = 16 * RT;
+  constexpr int STEP = KG * kTile;
+  constexpr int RB = D * (int)sizeof(T);
+  constexpr int kSlots = KG > 1 ? RG * KG / 2 : 1;
+  __shared__ __align__(16) f32x4 s_o[kSlots][KG > 1 ? RT * (D / 16) : 1][64];
+  __shared__ float2 s_ml[kSlots][RT][64];
+  const uint32_t bh = blockIdx.y, b = bh / (uint32_t)a.hkv;
+  const int head = bh - b * a.hkv;
+  const int split = blockIdx.x % a.splits, rb = blockIdx.x / a.splits;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+  int len, count;
+  if (!sequence_of(a.n, b, len, count)) return;
+  const int kw = wave % KG, rw = wave / KG;
+  const int nrows = count * a.G;
+  if (rb * RG * ROWS >= nrows) return;
+  const int row0 = (rb * RG + rw) * ROWS;
+  if (KG == 1 && row0 >= nrows) return;
+  const int end = len + count;
+  const int chunk = chunk_of(a, end);
+  const int e0 = split * chunk, e1 = min(e0 + chunk, end);
+  if (e0 >= e1) return;                  // behind a shorter sequence's end: the combining kernel does not read the slot
+
+  Rows<T, D, RT> rows;
+  const uint64_t anc = e1 > len ? ancestors(a.parent ? a.parent + (size_t)b * a.n.n : nullptr, a.n.n, lane) : 0;
+  load_rows<T, D, RT>(rows, a, b, head, row0, nrows, anc, col, grp);
+  RowTile<D> st[RT];
+  bool careful = false;
+  for (;;) {
+    clear<D, RT>(st);
+    int e = e0 + kw * kTile;
+    // Steps of entries that all rows attend to.  The next step's keys are loaded when this one's have become logits and
+    // its values when this one's are added, into the same registers.
+    int whole = min(e1, len);
+    if (!careful && e + kTile <= whole) {
+      PageWindow pages;
+      pages.fill(a.c, b, e >> a.c.shift, whole, lane);
+      if (e + kTile <= whole) {
+        Keys<T, D> k;
+        Values<T, D> v;
+        float p[RT][8];
+        k.load(a.c, a.hkv, head, e, pages.at(a.c, e + 8 * (col >> 2)), pages.at(a.c, e + 8 * grp), col, grp);
+        v.load(a.c, a.hkv, head, e, pages.at(a.c, e + 8 * grp), col, grp);
+        for (;;) {
+          const int next = e + STEP;
+          if (!pages.holds(a.c, next + kTile - 1)) pages.fill(a.c, b, next >> a.c.shift, whole, lane);
+          if (next + kTile > whole) break;
+          const int pk = pages.at(a.c, next + 8 * (col >> 2)), pv = pages.at(a.c, next + 8 * grp);
+          logits<T, D, RT>(p, k, rows, a.scale, a.c.bias != nullptr);
+          __builtin_amdgcn_sched_barrier(0);   // loads moved up would need registers of their own
+          k.load(a.c, a.hkv, head, next, pk, pv, col, grp);
+          __builtin_amdgcn_sched_barrier(0);
+          soften<sizeof(T) == 2, D, RT>(st, p, false);
+          add_values<T, D, RT>(st, v.v, p);
+          __builtin_amdgcn_sched_barrier(0);
+          v.load(a.c, a.hkv, head, next, pv, col, grp);
+          e = next;
+        }
+        logits<T, D, RT>(p, k, rows, a.scale, a.c.bias != nullptr);
+        soften<sizeof(T) == 2, D, RT>(st, p, false);
+        add_values<T, D, RT>(st, v.v, p);
+        e += STEP;
+      }
+    }
+    attend_edges<T, D, RT>(st, rows, a, b, head, e, e1, STEP, len, end, careful, col, grp);
+    if (careful || !__any(!all_finite<D, RT>(st))) break;
+    careful = true;
+  }
+  finish<T, D, RT, RG, KG>(st, s_o[0][0], s_ml[0][0], a, b, head, row0, nrows, split, rw, kw, lane);
+}
+
+// Calls with more than 32 rows a KV head: the waves of a workgroup share the entries in LDS.  A tile is 32 KG entries, K
+// rows, V rows and biases; two of them alternate, the one after the next is on its way in registers.  Every thread
+// moves 16-byte chunks, chunk i of the tile to place i of LDS, so that the swizzle is one of the addresses in memory.
+template <typename T, int D, int RG, int KG>
+__global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, 2>())) void tree_shared_kernel(TreeArgs a) {
+  constexpr int RT = 2;
+  constexpr int SUB = tiles_of_turn(KG);
+  constexpr int ROWS = 16 * RT, NT = RG * KG * 64, STEP = KG * SUB * kTile;
+  constexpr int RB = D * (int)sizeof(T), CH = RB / 16;
+  constexpr int kHalf = STEP * CH;                  // chunks of a tile's K rows
+  constexpr int kLoads = 2 * kHalf / NT;
+  static_assert(2 * kHalf % NT == 0 && kHalf % 64 == 0, "whole chunks a thread, K or V a wave");
+  constexpr int kTileBytes = 2 * STEP * RB + STEP * 4;
+  constexpr int kSlots = KG > 1 ? RG * KG / 2 : 0;
+  constexpr int kMergeBytes = kSlots * RT * 64 * ((D / 16) * 16 + 8);
+  __shared__ __align__(16) char lds[2 * kTileBytes > kMergeBytes ? 2 * kTileBytes : kMergeBytes];
+  const uint32_t bh = blockIdx.y, b = bh / (uint32_t)a.hkv;
+  const int head = bh - b * a.hkv;
+  const int split = blockIdx.x % a.splits, rb = blockIdx.x / a.splits;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+  int len, count;
+  if (!sequence_of(a.n, b, len, count)) return;
+  const int kw = wave % KG, rw = wave / KG;
+  const int nrows = count * a.G;
+  if (rb * RG * ROWS >= nrows) return;
+  const int row0 = (rb * RG + rw) * ROWS;
+  const bool idle = row0 >= nrows;                  // loads and waits with the others
+  const int end = len + count;
+  const int chunk = chunk_of(a, end);
+  const int e0 = split * chunk, e1 = min(e0 + chunk, end);
+  if (e0 >= e1) return;
+
+  Rows<T, D, RT> rows;
+  const uint64_t anc = e1 > len ? ancestors(a.parent ? a.parent + (size_t)b * a.n.n : nullptr, a.n.n, lane) : 0;
+  load_rows<T, D, RT>(rows, a, b, head, row0, nrows, anc, col, grp);
+  RowTile<D> st[RT];
+  bool careful = false;
+  const size_t page_rows = (size_t)a.hkv << a.c.shift, head_row = (size_t)head << a.c.shift;
+  const int mask = (1 << a.c.shift) - 1;
+  for (;;) {
+    clear<D, RT>(st);
+    int e = e0, whole = min(e1, len);
+    // Tiles of entries that all rows attend to.
+    if (!careful && e + STEP <= whole) {
+      PageWindow pages;
+      Chunk16 ahead[kLoads];
+      float bias_ahead = 0.f;
+      pages.fill(a.c, b, e >> a.c.shift, whole, lane);
+      // the tile at `from` into registers; the rows of a wave's chunks are on one page
+      const auto fetch = [&](int from) {
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));   // places formed anew: kept from turn to turn they cost more registers than there are
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int at = (tid + i * NT) % kHalf, row = at / CH;
+          const int first = (wave * 64 + i * NT) % kHalf / CH;
+          const int page = __builtin_amdgcn_readlane(pages.page, ((from + first) >> a.c.shift) - pages.first);
+          const char* rows0 = ((wave * 64 + i * NT) / kHalf ? a.c.V : a.c.K) +
+                              ((size_t)page * page_rows + head_row + ((from + first) & mask & ~7)) * RB;
+          ahead[i] = load16(rows0 + (row - (first & ~7)) * RB + ((at % CH ^ swizzle(row)) << 4));
+        }
+        if (a.c.bias && (int)threadIdx.x < STEP) {
+          const int page = __shfl(pages.page, ((from + tid) >> a.c.shift) - pages.first, 64);
+          bias_ahead = a.c.bias[(size_t)page * page_rows + head_row + ((from + tid) & mask)];
+        }
+      };
+      // whether the tile at `from` is one of those
+      const auto more = [&](int from) {
+        if (from + STEP <= whole && !pages.holds(a.c, from + STEP - 1)) pages.fill(a.c, b, from >> a.c.shift, whole, lane);
+        return from + STEP <= whole;
+      };
+      const auto put = [&](char* tile) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) store16(tile + (threadIdx.x + i * NT) * 16, ahead[i]);
+        if ((int)threadIdx.x < STEP) reinterpret_cast<float*>(tile + 2 * STEP * RB)[threadIdx.x] = bias_ahead;
+      };
+      const Places<T, D> places(col, grp);
+      bool here = more(e);
+      if (here) {
+        fetch(e);
+        put(lds);
+      }
+      bool next = here && more(e + STEP);
+      if (next) fetch(e + STEP);
+      __syncthreads();
+      for (int turn = 0; here; turn ^= 1) {
+        const char* tile = lds + turn * kTileBytes;
+        if (next) put(lds + (turn ^ 1) * kTileBytes);
+        const bool after = next && more(e + 2 * STEP);
+        if (after) fetch(e + 2 * STEP);
+        if (!idle) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+          const int sub = u * KG + kw;
+          float p[RT][8];
+          Keys<T, D> k;
+          read_keys<T, D>(k, tile + sub * kTile * RB, tile + 2 * STEP * RB + sub * kTile * 4, places);
+          logits<T, D, RT>(p, k, rows, a.scale, true);
+          Values<T, D> v;
+          read_values<T, D>(v, tile + (STEP + sub * kTile) * RB, places);
+          soften<sizeof(T) == 2, D, RT>(st, p, false);
+          add_values<T, D, RT>(st, v.v, p);
+        }
+        }
+        __syncthreads();
+        e += STEP;
+        here = next;
+        next = after;
+      }
+    }
+    if (!idle) attend_edges<T, D, RT>(st, rows, a, b, head, e + kw * kTile, e1, KG * kTile, len, end, careful, col, grp);
+    if (careful || !__syncthreads_or(!idle && !all_finite<D, RT>(st))) break;
+    careful = true;
+  }
+  f32x4* s_o = reinterpret_cast<f32x4*>(lds);
+  finish<T, D, RT, RG, KG>(st, s_o, reinterpret_cast<float2*>(s_o + kSlots * RT * (D / 16) * 64), a, b, head, row0, nrows,
+                           split, rw, kw, lane);
+}
+
+// Combines the partials of the rows, in slot order.  A unit of d/4 threads takes four channels each of the slots sub,
+// sub + SUB, ... of a row and loads kBatch of them at a time; with SUB > 1 all units of a workgroup share a row and
+// meet in LDS, in order.
+template <typename T, int D, int SUB>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, uint32_t rows) {
   constexpr int kUnits = 256 / (D / 4);
+  constexpr int kBatch = 8;
+  static_assert(SUB == 1 || SUB == kUnits, "a unit is a row, or all of them are one");
+  __shared__ float2 s_ml[kUnits];
+  __shared__ __align__(16) f32x4 s_o[kUnits][D / 4];
   const uint32_t per = (uint32_t)a.n.n * a.G;
-  const uint32_t row = blockIdx.x * kUnits + threadIdx.x / (D / 4);
-  const int c4 = threadIdx.x % (D / 4);
+  const int c4 = threadIdx.x % (D / 4), unit = threadIdx.x / (D / 4), sub = SUB == 1 ? 0 : unit;
+  const uint32_t row = SUB == 1 ? blockIdx.x * kUnits + unit : blockIdx.x;
   if (row >= rows) return;
   const uint32_t bh = row / per, r = row - bh * per, b = bh / (uint32_t)a.hkv, head = bh - b * a.hkv;
   int len, count;
   if (!sequence_of(a.n, b, len, count)) return;
   const uint32_t node = r / (uint32_t)a.G, g = r - node * a.G;
   if ((int)node >= count) return;
-  const int end = len + count, chunk = chunk_of(a.splits, end), slots = (end + chunk - 1) / chunk;
+  const int end = len + count, chunk = chunk_of(a, end), slots = (end + chunk - 1) / chunk;
+  const size_t part = (size_t)bh * a.splits * per + r;
   float m = kNegInf, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < slots; ++s) {
-    const size_t part = ((size_t)bh * a.splits + s) * per + r;
-    const float2 ml = a.part_ml[part];
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + part * D + 4 * c4);
-    if (ml.x == kNegInf) continue;
-    const float M = fmaxf(m, ml.x);
-    const float c0 = weight_of(m, M), c1 = weight_of(ml.x, M);
-    l = l * c0 + ml.y * c1;
+  for (int s0 = sub; s0 < slots; s0 += SUB * kBatch) {
+    f32x4 x[kBatch];
+    float2 ml[kBatch];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = o[k] * c0 + x[k] * c1;
+    for (int u = 0; u < kBatch; ++u) {
+      const size_t at = part + (size_t)min(s0 + u * SUB, slots - 1) * per;
+      x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * c4);
+      ml[u] = a.part_ml[at];
+    }
+    float M = m;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (s0 + u * SUB >= slots) ml[u].x = kNegInf;
+      M = fmaxf(M, ml[u].x);
+    }
+    const float c = weight_of(m, M);
+    l *= c;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] *= c;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const bool some = ml[u].x != kNegInf;             // a part that nothing counts in may be NaN
+      const float w = weight_of(ml[u].x, M);
+      l = some ? fmaf(ml[u].y, w, l) : l;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = some ? fmaf(x[u][k], w, o[k]) : o[k];
+    }
     m = M;
+  }
+  if constexpr (SUB > 1) {
+    s_o[unit][c4] = o;
+    if (c4 == 0) s_ml[unit] = make_float2(m, l);
+    __syncthreads();
+    if (unit > 0) return;
+    float M = kNegInf;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) M = fmaxf(M, s_ml[u].x);
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const float2 ml = s_ml[u];
+      const bool some = ml.x != kNegInf;
+      const float w = weight_of(ml.x, M);
+      const f32x4 x = s_o[u][c4];
+      l = some ? fmaf(ml.y, w, l) : l;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = some ? fmaf(x[k], w, o[k]) : o[k];
+    }
   }
   Chunk16 w = zero16();
 #pragma unroll
@@ -480,12 +844,28 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a, uint32_t 
 
 template <typename T, int D>
 hipError_t launch_td(int64_t heads, const TreePlan& plan, const TreeArgs& a, hipStream_t st) {
-  const dim3 grid(a.splits * a.row_blocks, (unsigned)heads), blk(kThreads);
-  hipLaunchKernelGGL((tree_kernel<T, D, 1>), grid, blk, 0, st, a);
+  const dim3 grid(a.splits * a.row_blocks, (unsigned)heads);
+  const auto with = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * plan.row_groups * plan.key_groups), 0, st, a);
+  };
+  constexpr bool kWide = sizeof(T) == 4 && D == 128;   // registers for half as many waves
+  if (plan.row_tiles == 1) with(tree_kernel<T, D, 1, 1, 4>);
+  else if (plan.row_groups == 1) with(tree_kernel<T, D, 2, 1, 4>);
+  else if constexpr (kWide) {
+    if (plan.row_groups == 2) with(tree_shared_kernel<T, D, 2, 2>);
+    else with(tree_shared_kernel<T, D, 4, 1>);
+  } else {
+    if (plan.row_groups == 2) with(tree_shared_kernel<T, D, 2, 4>);
+    else if (plan.row_groups == 4) with(tree_shared_kernel<T, D, 4, 2>);
+    else with(tree_shared_kernel<T, D, 8, 1>);
+  }
   if (a.splits > 1) {
     const uint32_t rows = (uint32_t)heads * a.n.n * a.G;
     constexpr int kUnits = 256 / (D / 4);
-    hipLaunchKernelGGL((tree_combine_kernel<T, D>), dim3((rows + kUnits - 1) / kUnits), blk, 0, st, a, rows);
+    if (a.splits <= kFewSlots)
+      hipLaunchKernelGGL((tree_combine_kernel<T, D, 1>), dim3((rows + kUnits - 1) / kUnits), dim3(256), 0, st, a, rows);
+    else
+      hipLaunchKernelGGL((tree_combine_kernel<T, D, kUnits>), dim3(rows), dim3(256), 0, st, a, rows);
   }
   return hipGetLastError();
 }
@@ -500,20 +880,61 @@ size_t parts_bytes(int64_t heads, int splits, int rows, int d, size_t* ml_off) {
 
 }  // namespace
 
-TreePlan plan_tree(int64_t heads, int entries, int d, int rows, size_t) {
+namespace {
+
+// Most splits of a head: kMaxRounds rounds of workgroups.
+int most_splits(int64_t units, int entries, int step) {
+  const int64_t rounds = std::max<int64_t>(1, (int64_t)kMaxRounds * kCUs / units);
+  return (int)std::min<int64_t>({rounds, (int64_t)kMaxSplit, ((int64_t)entries + step - 1) / step});
+}
+
+TreePlan plan_rows(int64_t heads, int d, int rows, size_t elem) {
   TreePlan p;
-  p.row_tiles = 1;
-  p.split_rows = false;
-  p.row_blocks = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
-  const int64_t want = std::max<int64_t>(1, kTargetBlocks / (heads * p.row_blocks));
-  p.splits = (int)std::min<int64_t>({want, (int64_t)kMaxSplit, ((int64_t)entries + kStep - 1) / kStep});
+  const int tiles = (rows + 15) / 16;
+  const bool wide = elem == 4 && d == 128;   // registers for half as many waves
+  p.row_tiles = tiles == 1 ? 1 : 2;
+  p.row_groups = tiles <= 2 ? 1 : tiles <= 4 ? 2 : tiles <= 8 || wide ? 4 : 8;
+  p.key_groups = (p.row_groups == 1 || wide ? 4 : 8) / p.row_groups;
+  const int per = p.row_tiles * p.row_groups;
+  p.row_blocks = (tiles + per - 1) / per;
+  p.step = p.key_groups * kTile * (p.row_groups > 1 ? tiles_of_turn(p.key_groups) : 1);
+  return p;
+}
+
+}  // namespace
+
+// How the entries are divided.  A CU reads and computes at one rate however many workgroups share it, so a call takes
+// the entries of a workgroup, and what one costs besides, times the workgroups of the fullest CU: one layer of 25605
+// entries (8 heads, 5 nodes) takes 27.6 us in 29 splits, one workgroup on most CUs, and 29.2 in 51, two on some; 64
+// nodes 78 in 31 and 101 in 51.  Where lengths are the device's to know, three rounds: 16 sequences of 0 to 8100
+// entries (26 nodes, 8 heads) take 154 us in 6 splits, 163 in 4 and 196 in 2.
+TreePlan plan_tree(int64_t heads, int entries, int d, int rows, size_t elem, bool ragged) {
+  TreePlan p = plan_rows(heads, d, rows, elem);
+  const int64_t units = heads * p.row_blocks;
+  const int most = most_splits(units, entries, p.step);
+  p.splits = 1;
+  if (ragged) {
+    p.splits = (int)std::min<int64_t>(most, std::max<int64_t>(1, (int64_t)kRaggedRounds * kCUs / units));
+  } else {
+    int64_t best = INT64_MAX;
+    for (int s = 1; s <= most; ++s) {
+      const int64_t chunk = ((entries + s - 1) / s + p.step - 1) / p.step * p.step;
+      const int64_t groups = (entries + chunk - 1) / chunk * units;
+      const int64_t cost = (groups + kCUs - 1) / kCUs * (chunk + kGroupCost) + (s > 1 ? kCombineCost : 0);
+      if (cost < best) best = cost, p.splits = s;
+    }
+  }
   p.bytes = parts_bytes(heads, p.splits, rows, d, &p.ml_off);
   return p;
 }
 
 size_t tree_workspace_bound(int64_t heads, int capacity, int d, int G, int n, size_t elem) {
   size_t most = 0;   // fewer nodes may take more splits
-  for (int i = 1; i <= n; ++i) most = std::max(most, plan_tree(heads, capacity, d, i * G, elem).bytes);
+  for (int i = 1; i <= n; ++i) {
+    const TreePlan p = plan_rows(heads, d, i * G, elem);
+    size_t ml_off;
+    most = std::max(most, parts_bytes(heads, most_splits(heads * p.row_blocks, capacity, p.step), i * G, d, &ml_off));
+  }
   return most;
 }
 
@@ -532,6 +953,7 @@ hipError_t launch_tree_attn(int batch, int hkv, int d, int G, int dtype, float s
   a.G = G;
   a.splits = plan.splits;
   a.row_blocks = plan.row_blocks;
+  a.step = plan.step;
   a.scale = scale;
   const int64_t heads = (int64_t)batch * hkv;
   if (dtype == SELKV_BF16)
