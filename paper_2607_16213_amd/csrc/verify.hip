@@ -10,12 +10,13 @@
 //
 // Sums are fp64: the drawn token is the first whose sum of weights passes a
 // threshold, and rounded to fp32 the sums of 100000 weights would move that
-// border past tokens as likely as 1e-6.  A sum is taken in chunks of 2048 tokens,
+// border past tokens as likely as 1e-6.  A sum is taken in chunks of 1024 tokens,
 // each by one wave in a fixed order; a token is drawn by finding its chunk, then
 // its place there.
 //
-// One workgroup of sixteen waves takes a sequence.  Every wave holds the nodes,
-// one per lane, and walks by itself.
+// A sum needs the walk before it, so they take turns: each launch of sum_kernel walks on from what the last one summed
+// (every wave by itself, one node per lane) and sums the next chunk after, over all CUs; draw_kernel, one workgroup a
+// sequence, finishes, by itself where more sums are left than launches, and draws.
 #include <algorithm>
 
 #include "common.hpp"
@@ -24,14 +25,27 @@
 namespace selkv {
 namespace {
 
-constexpr int kWaves = 16;
+constexpr int kWaves = 16;                   // of draw_kernel
 constexpr int kThreads = kWaves * 64;
-constexpr int kChunk = 2048;                 // tokens of a sum
+constexpr int kSumWaves = 4;                 // of sum_kernel: a chunk each
+constexpr int kChunk = 1024;                 // tokens of a sum
 constexpr int kMaxVocab = 1 << 21;
 constexpr int kMaxChunks = kMaxVocab / kChunk + 1;
+constexpr int kMaxNodes = 64;
+
+// A walk between two launches.
+struct Walk {
+  double c, mass;          // the residual is max(p - c q, 0) / mass
+  uint64_t taken, todo, out;   // nodes accepted; children of `at` to be tried; nodes whose tokens are taken out
+  int at;
+  int wants;               // what sum comes next
+  int parts;               // the launch that summed what the walk stands on
+  int pad;
+};
+enum { kRefusal, kLast, kNothing };   // mass of the residual; of what the token is drawn from; the walk is over
 
 struct VerifyArgs {
-  int n, vocab;
+  int n, vocab, chunks;    // chunks: room for a row's
   const int32_t* tokens;
   const int32_t* parent;
   const char* target;
@@ -41,6 +55,11 @@ struct VerifyArgs {
   int32_t* path;
   int32_t* n_path;
   int32_t* next;
+  // workspace, B of each in turn: walks and sums of every launch, the nodes' probabilities
+  Walk* walks;
+  double* parts;
+  float2* probs;           // [B, 64]
+  int batch, launches;
 };
 
 __device__ __forceinline__ double sum64(double v) {
@@ -76,11 +95,12 @@ __device__ __forceinline__ double prob(const char* row, int x) {
   else return (double)reinterpret_cast<const float*>(row)[x];
 }
 
-// The rows of one node.  A row of odd length starts anywhere, so chunks count from the 16-byte boundary at or before it:
-// place x + shift of the row is place x of the aligned one.
+// The rows of one node.  A row of odd length starts anywhere, so places count from the 16-byte boundary at or before it:
+// token x is at place x + shift.
 template <typename T>
 struct Dist {
   static constexpr int N = Elem<T>::kPerChunk;
+  static constexpr int kSteps = kChunk / (64 * N);
   const char* p;       // aligned down
   const char* q;       // nullptr: no draft
   int shift, vocab;
@@ -88,81 +108,110 @@ struct Dist {
   uint64_t out;        // nodes whose tokens are taken out (without a draft)
   int token;           // of the lane's node
 
-  // N places of a row from `at` (a multiple of N); those behind its end are not read
-  __device__ __forceinline__ Chunk16 load(const char* row, int at) const {
-    if (at + N <= places()) return load16(row + (size_t)at * sizeof(T));
-    Chunk16 r = zero16();
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (at + e < places()) Elem<T>::put(r, e, (float)prob<T>(row, at + e));
-    return r;
-  }
+  __device__ __forceinline__ int places() const { return vocab + shift; }
+  __device__ __forceinline__ int chunks() const { return (places() + kChunk - 1) / kChunk; }
 
-  // weights of the N places from `at` (a multiple of N)
-  __device__ __forceinline__ void weights(int at, double (&w)[N]) const {
-    const Chunk16 a = load(p, at);
-    const Chunk16 b = q ? load(q, at) : zero16();
+  // Weights of a chunk's places, 64 N a step, lane by lane.  Whole blocks of N by 16-byte loads, all in flight together;
+  // the few places behind the last whole block, which lie at the row's end, one a lane as a step of their own.
+  struct Weights {
+    Chunk16 a[kSteps], b[kSteps];
+    double tail;
+  };
+  __device__ __forceinline__ int whole() const { return places() / N * N; }
+  __device__ __forceinline__ int tail_at(int lane) const { return whole() + lane; }
+  __device__ __forceinline__ bool has_tail(int chunk) const { return chunk == chunks() - 1 && whole() < places(); }
+  __device__ __forceinline__ void load(Weights& w, int chunk, int lane) const {
+    const int at0 = chunk * kChunk + lane * N;
+    if (whole() > 0) {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) w.a[s] = load16(p + (size_t)min(at0 + s * 64 * N, whole() - N) * sizeof(T));
+      if (q) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) w.b[s] = load16(q + (size_t)min(at0 + s * 64 * N, whole() - N) * sizeof(T));
+      }
+    }
+    w.tail = 0.0;
+    if (has_tail(chunk) && tail_at(lane) < places() && tail_at(lane) >= shift) {
+      const int at = tail_at(lane);
+      w.tail = left_of(prob<T>(p, at), q ? prob<T>(q, at) : 0.0, c);
+    }
+    if (out && has_tail(chunk)) w.tail = taken_out(tail_at(lane)) ? 0.0 : w.tail;
+  }
+  __device__ __forceinline__ bool taken_out(int place) const {
+    bool is = false;
+    for (uint64_t some = out; some; some &= some - 1) {
+      const int x = __shfl(token, __ffsll((unsigned long long)some) - 1, 64);   // by all lanes
+      is |= x + shift == place;
+    }
+    return is;
+  }
+  __device__ __forceinline__ void step(const Weights& w, int s, int chunk, int lane, double (&x)[N]) const {
+    const int at = chunk * kChunk + s * 64 * N + lane * N;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const int x = at + e - shift;
-      w[e] = (uint32_t)x < (uint32_t)vocab ? left_of((double)Elem<T>::get(a, e), (double)Elem<T>::get(b, e), c) : 0.0;
+      const bool there = at < whole() && at + e >= shift;
+      x[e] = there ? left_of((double)Elem<T>::get(w.a[s], e), q ? (double)Elem<T>::get(w.b[s], e) : 0.0, c) : 0.0;
     }
-    uint64_t some = out;                 // few, and only without a draft
-    while (some) {
-      const int i = __ffsll((unsigned long long)some) - 1;
-      some &= some - 1;
-      const int x = __shfl(token, i, 64) + shift - at;
+    if (out) {
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (x == e) w[e] = 0.0;
+        if (taken_out(at + e)) x[e] = 0.0;
     }
   }
-  __device__ __forceinline__ int places() const { return vocab + shift; }
 
   // Weights of a chunk, added up: every lane its own, then across.
   __device__ __forceinline__ double sum(int chunk, int lane) const {
-    double s = 0.0;
-    const int end = min((chunk + 1) * kChunk, places());
-    for (int at0 = chunk * kChunk; at0 < end; at0 += 64 * N) {
-      const int at = at0 + lane * N;
-      double w[N];
-      weights(min(at, (places() - 1) / N * N), w);
+    Weights w;
+    load(w, chunk, lane);
+    double total = w.tail;
 #pragma unroll
-      for (int e = 0; e < N; ++e) s += at < end ? w[e] : 0.0;
+    for (int s = 0; s < kSteps; ++s) {
+      double x[N];
+      step(w, s, chunk, lane, x);
+#pragma unroll
+      for (int e = 0; e < N; ++e) total += x[e];
     }
-    return sum64(s);
+    return sum64(total);
   }
 
   // The first token of the chunk at which the sum from `before` on exceeds `limit`, or the chunk's last with a weight.
   __device__ __forceinline__ int find(int chunk, double before, double limit, int lane) const {
-    const int end = min((chunk + 1) * kChunk, places());
+    Weights w;
+    load(w, chunk, lane);
     int last = -1;
-    for (int at0 = chunk * kChunk; at0 < end; at0 += 64 * N) {
-      const int at = at0 + lane * N;
-      double w[N];
-      weights(min(at, (places() - 1) / N * N), w);
+#pragma unroll
+    for (int s = 0; s <= kSteps; ++s) {
+      if (s == kSteps && !has_tail(chunk)) break;
+      const int at = s < kSteps ? chunk * kChunk + s * 64 * N + lane * N : tail_at(lane);
+      double x[N];
+      if (s < kSteps) {
+        step(w, s, chunk, lane, x);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = e == 0 ? w.tail : 0.0;
+      }
       double own = 0.0;
       int mine = -1;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        if (at >= end) w[e] = 0.0;
-        own += w[e];
-        if (w[e] > 0.0) mine = at + e - shift;
+        own += x[e];
+        if (x[e] > 0.0) mine = at + e - shift;
       }
       const double upto = before + scan64(own, lane);
       const uint64_t past = __ballot(upto > limit && mine >= 0);
       if (past) {
-        const int at_lane = __ffsll((unsigned long long)past) - 1;
         double run = upto - own;
-        int x = mine;
+        int found = mine;      // the lane's last with a weight if none by rounding
+        bool open = true;
 #pragma unroll
-        for (int e = N - 1; e >= 0; --e) {   // the first place whose sum is past the limit; the lane's last if none by rounding
-          double t = run;
-#pragma unroll
-          for (int k = 0; k <= e; ++k) t += w[k];
-          if (t > limit && w[e] > 0.0) x = at + e - shift;
+        for (int e = 0; e < N; ++e) {
+          run += x[e];
+          if (open && run > limit && x[e] > 0.0) {
+            found = at + e - shift;
+            open = false;
+          }
         }
-        return __shfl(x, at_lane, 64);
+        return __shfl(found, __ffsll((unsigned long long)past) - 1, 64);
       }
       const uint64_t some = __ballot(mine >= 0);
       if (some) last = __shfl(mine, 63 - __clzll((long long)some), 64);
@@ -172,8 +221,151 @@ struct Dist {
   }
 };
 
+// A sequence's nodes, one per lane, and the walk over them.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
+struct Walker {
+  size_t node0, row_bytes;
+  const VerifyArgs* a;
+  int token, up, lane;
+  double u, p, q;
+  Walk s;
+  Dist<T> dist;
+
+  // `probs`: of the nodes, where a launch before has gathered them
+  __device__ __forceinline__ void load(const VerifyArgs& args, uint32_t b, int count, int lane_, const float2* probs) {
+    a = &args;
+    lane = lane_;
+    node0 = (size_t)b * a->n;
+    row_bytes = (size_t)a->vocab * sizeof(T);
+    token = up = -1;
+    u = p = q = 0.0;
+    if (lane < count) {
+      token = a->tokens[node0 + lane];
+      up = a->parent ? a->parent[node0 + lane] : lane - 1;
+      u = a->u[node0 + lane];
+      if ((uint32_t)up >= (uint32_t)lane) up = -1;
+      if ((uint32_t)token >= (uint32_t)a->vocab) token = -1;
+      if (probs) {
+        p = probs[lane].x;
+        q = probs[lane].y;
+      } else if (up >= 0 && token >= 0) {
+        p = prob<T>(a->target + (node0 + up) * row_bytes, token);
+        q = a->draft ? prob<T>(a->draft + (node0 + up) * row_bytes, token) : 1.0;
+      }
+    }
+    dist.vocab = a->vocab;
+    dist.token = token;
+  }
+  __device__ __forceinline__ void begin() {
+    s.c = 0.0;
+    s.mass = 1.0;
+    s.taken = 1;
+    s.out = 0;
+    s.todo = __ballot(up == 0);
+    s.at = 0;
+    s.parts = -1;
+  }
+  // The walk up to the next sum.  summed: mass is that of the residual here.
+  __device__ __forceinline__ void walk(bool summed) {
+    s.wants = kLast;
+    while (s.todo) {
+      const int i = __ffsll((unsigned long long)s.todo) - 1;
+      s.todo &= s.todo - 1;
+      const double pi = __shfl(p, i, 64), qi = __shfl(q, i, 64), ui = __shfl(u, i, 64);
+      const int xi = __shfl(token, i, 64);
+      // without a draft q is 1, and a token refused before has nothing left
+      const double w = a->draft ? left_of(pi, qi, s.c) : (__ballot(token == xi) & s.out) || !(pi > 0.0) ? 0.0 : pi;
+      if (xi >= 0 && threshold(ui, qi, s.mass) < w) {
+        s.at = i;
+        s.taken |= 1ull << i;
+        s.c = 0.0;
+        s.mass = 1.0;
+        s.out = 0;
+        s.todo = __ballot(up == i);
+        summed = false;
+      } else if (a->draft) {
+        if (s.mass > 0.0) {                    // with nothing left every other child is refused too
+          s.c += s.mass;
+          s.wants = kRefusal;
+          return;
+        }
+      } else if (xi >= 0) {
+        s.mass = fmax(s.mass - w, 0.0);
+        s.out |= 1ull << i;
+      }
+    }
+    if (summed) last(s.mass);
+  }
+  // The mass of what the token is drawn from: of the target itself where nothing is left of it.
+  __device__ __forceinline__ void last(double all) {
+    s.mass = all;
+    s.wants = kNothing;
+    if (!(all > 0.0) && (s.c != 0.0 || s.out)) {
+      s.c = 0.0;
+      s.out = 0;
+      s.wants = kLast;
+    }
+  }
+  // On from a sum.
+  __device__ __forceinline__ void resume(double sum) {
+    if (s.wants == kLast) {
+      last(sum);
+    } else if (s.wants == kRefusal) {
+      s.mass = sum;
+      walk(true);
+    }
+  }
+  __device__ __forceinline__ void stand() {
+    const size_t at = (node0 + s.at) * row_bytes;
+    dist.shift = (int)(at % 16 / sizeof(T));
+    dist.p = a->target + at / 16 * 16;
+    dist.q = a->draft ? a->draft + at / 16 * 16 : nullptr;
+    dist.c = s.c;
+    dist.out = s.out;
+  }
+  // A row's chunks added up, in the same order wherever they were summed.
+  template <typename P>
+  __device__ __forceinline__ double total(const P* parts, int chunks) const {
+    double t = 0.0;
+    for (int i0 = 0; i0 < chunks; i0 += 64) t += sum64(i0 + lane < chunks ? parts[i0 + lane] : 0.0);
+    return t;
+  }
+};
+
+// Walks on from launch r - 1 and sums the next of what is wanted, a chunk a wave.
+template <typename T>
+__global__ __launch_bounds__(kSumWaves * 64) void sum_kernel(VerifyArgs a, int r) {
+  const uint32_t b = blockIdx.y;
+  const int lane = threadIdx.x & 63, chunk = blockIdx.x * kSumWaves + (threadIdx.x >> 6);
+  const int count = a.counts ? a.counts[b] : a.n;
+  if (count < 1 || count > a.n) return;
+  Walker<T> w;
+  w.load(a, b, count, lane, r ? a.probs + (size_t)b * kMaxNodes : nullptr);
+  if (r == 0) {
+    w.begin();
+    w.walk(false);
+  } else {
+    w.s = a.walks[(size_t)(r - 1) * a.batch + b];
+    if (w.s.wants != kNothing) {
+      w.stand();
+      w.resume(w.total(a.parts + ((size_t)(r - 1) * a.batch + b) * a.chunks, w.dist.chunks()));
+    }
+  }
+  w.stand();
+  const bool sums = w.s.wants != kNothing;
+  if (sums) w.s.parts = r;
+  if (sums && chunk < w.dist.chunks()) {
+    const double s = w.dist.sum(chunk, lane);
+    if (lane == 0) a.parts[((size_t)r * a.batch + b) * a.chunks + chunk] = s;
+  }
+  if (chunk == 0) {
+    if (lane == 0) a.walks[(size_t)r * a.batch + b] = w.s;
+    if (r == 0) a.probs[(size_t)b * kMaxNodes + lane] = make_float2((float)w.p, (float)w.q);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void draw_kernel(VerifyArgs a) {
   __shared__ double s_part[kMaxChunks];
   const uint32_t b = blockIdx.x;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -184,94 +376,43 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
     if (threadIdx.x == 0) a.n_path[b] = 0, a.next[b] = -1;
     return;
   }
-  const size_t node0 = (size_t)b * a.n;
-  const size_t row_bytes = (size_t)a.vocab * sizeof(T);
-  // lane i: node i
-  int token = -1, up = -1;
-  double u = 0.0, p = 0.0, q = 0.0;
-  if (lane < count) {
-    token = a.tokens[node0 + lane];
-    up = a.parent ? a.parent[node0 + lane] : lane - 1;
-    u = a.u[node0 + lane];
-    if ((uint32_t)up >= (uint32_t)lane) up = -1;
-    if ((uint32_t)token >= (uint32_t)a.vocab) token = -1;
-    if (up >= 0 && token >= 0) {
-      p = prob<T>(a.target + (node0 + up) * row_bytes, token);
-      q = a.draft ? prob<T>(a.draft + (node0 + up) * row_bytes, token) : 1.0;
+  const int r = a.launches;
+  Walker<T> w;
+  w.load(a, b, count, lane, r ? a.probs + (size_t)b * kMaxNodes : nullptr);
+  if (r == 0) {
+    w.begin();
+    w.walk(false);
+    w.stand();
+  } else {
+    w.s = a.walks[(size_t)(r - 1) * a.batch + b];
+    w.stand();
+    if (w.s.wants != kNothing) {
+      w.resume(w.total(a.parts + ((size_t)(r - 1) * a.batch + b) * a.chunks, w.dist.chunks()));
+      w.stand();
     }
   }
-
-  Dist<T> dist;
-  dist.vocab = a.vocab;
-  dist.token = token;
-  const auto stand_on = [&](int node) {
-    const size_t at = (node0 + node) * row_bytes;
-    dist.shift = (int)(at % 16 / sizeof(T));
-    dist.p = a.target + at / 16 * 16;
-    dist.q = a.draft ? a.draft + at / 16 * 16 : nullptr;
-    dist.c = 0.0;
-    dist.out = 0;
-  };
-  // the sum of what dist says, by all waves; the chunks' sums stay in s_part
-  const auto total = [&]() {
-    const int chunks = (dist.places() + kChunk - 1) / kChunk;
-    __syncthreads();
+  bool here = false;                          // s_part holds the sums
+  while (w.s.wants != kNothing) {
+    const int chunks = w.dist.chunks();
     for (int i = wave; i < chunks; i += kWaves) {
-      const double s = dist.sum(i, lane);
+      const double s = w.dist.sum(i, lane);
       if (lane == 0) s_part[i] = s;
     }
     __syncthreads();
-    double s = 0.0;
-    for (int i0 = 0; i0 < chunks; i0 += 64) s += sum64(i0 + lane < chunks ? s_part[i0 + lane] : 0.0);
-    return s;
-  };
-
-  int at = 0;
-  uint64_t taken = 1;
-  double mass = 1.0;
-  bool summed = false;                        // s_part holds the weights of dist
-  stand_on(0);
-  uint64_t todo = __ballot(up == 0);          // children still to be tried
-  while (todo) {
-    const int i = __ffsll((unsigned long long)todo) - 1;
-    todo &= todo - 1;
-    const double pi = __shfl(p, i, 64), qi = __shfl(q, i, 64), ui = __shfl(u, i, 64);
-    const int xi = __shfl(token, i, 64);
-    // without a draft q is 1, and a token refused before has nothing left
-    const double w = a.draft ? left_of(pi, qi, dist.c)
-                             : (__ballot(token == xi) & dist.out) || !(pi > 0.0) ? 0.0 : pi;
-    if (xi >= 0 && threshold(ui, qi, mass) < w) {
-      at = i;
-      taken |= 1ull << i;
-      mass = 1.0;
-      summed = false;
-      stand_on(i);
-      todo = __ballot(up == i);
-    } else if (a.draft) {
-      if (mass > 0.0) {                        // with nothing left every other child is refused too
-        dist.c += mass;
-        mass = total();
-        summed = true;
-      }
-    } else if (xi >= 0) {
-      mass = fmax(mass - w, 0.0);
-      dist.out |= 1ull << i;
-    }
-  }
-  double all = summed ? mass : total();
-  if (!(all > 0.0) && (dist.c != 0.0 || dist.out)) {
-    dist.c = 0.0;
-    dist.out = 0;
-    all = total();
+    w.resume(w.total(s_part, chunks));
+    w.stand();
+    __syncthreads();
+    here = true;
   }
   if (wave > 0) return;
   // the chunk in which the sum passes the limit; the last with a weight if none by rounding
-  const double limit = __shfl(u, 0, 64) * all;
-  const int chunks = (dist.places() + kChunk - 1) / kChunk;
+  const double limit = __shfl(w.u, 0, 64) * w.s.mass;
+  const int chunks = w.dist.chunks();
+  const double* parts = a.parts + ((size_t)(here ? 0 : w.s.parts) * a.batch + b) * a.chunks;
   double before = 0.0, found_before = 0.0;
   int found = -1;
   for (int i0 = 0; i0 < chunks; i0 += 64) {
-    const double own = i0 + lane < chunks ? s_part[i0 + lane] : 0.0;
+    const double own = i0 + lane < chunks ? (here ? s_part[i0 + lane] : parts[i0 + lane]) : 0.0;
     const double upto = before + scan64(own, lane);
     const uint64_t past = __ballot(upto > limit && own > 0.0), some = __ballot(own > 0.0);
     const int pick = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : -1;
@@ -282,29 +423,63 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
     if (past) break;
     before = __shfl(upto, 63, 64);
   }
-  const int token_drawn = found < 0 ? -1 : dist.find(found, found_before, limit, lane);
+  const int token = found < 0 ? -1 : w.dist.find(found, found_before, limit, lane);
   int mine = -1, k = 0;
-  for (uint64_t rest = taken; rest; rest &= rest - 1, ++k)
+  for (uint64_t rest = w.s.taken; rest; rest &= rest - 1, ++k)
     if (lane == k) mine = __ffsll((unsigned long long)rest) - 1;
   if (lane < a.n) path[lane] = mine;
   if (lane == 0) {
-    a.n_path[b] = __popcll(taken);
-    a.next[b] = token_drawn;
+    a.n_path[b] = __popcll(w.s.taken);
+    a.next[b] = token;
   }
+}
+
+size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct VerifyPlan {
+  int launches, chunks;
+  size_t parts_off, probs_off, bytes;
+};
+
+// Launches of sum_kernel.  None where draw_kernel's sixteen waves take a row's chunks at once.  One where a walk has one
+// sum, a chain or children without a distribution: 32000 tokens 9.7 us, 11.3 without; 131072 10.4 us, 23.7 without.
+// Elsewhere a sum left over costs draw_kernel 1 us for 9000 tokens, a launch 2 us whether it is needed or not: 32 trees
+// of 26 nodes, 131072 tokens, 29 us with three, 44 with two, 32 with four; eight of 64 nodes 26 with four, 35 with three.
+VerifyPlan plan_verify(int batch, int n, int vocab, bool one_sum) {
+  VerifyPlan p;
+  p.chunks = (vocab + 7 + kChunk - 1) / kChunk;   // from the boundary before the row
+  const int most = one_sum || vocab <= (1 << 15) ? 1 : vocab <= (1 << 16) ? 2 : n <= 32 ? 3 : 4;
+  p.launches = p.chunks <= kWaves ? 0 : std::min(n, most);
+  const size_t walks = (size_t)p.launches * batch * sizeof(Walk);
+  p.parts_off = round256(walks);
+  p.probs_off = p.parts_off + round256((size_t)p.launches * batch * p.chunks * sizeof(double));
+  p.bytes = p.launches ? p.probs_off + (size_t)batch * kMaxNodes * sizeof(float2) : 0;
+  return p;
+}
+
+template <typename T>
+hipError_t launch_t(const VerifyArgs& a, hipStream_t st) {
+  for (int r = 0; r < a.launches; ++r)
+    hipLaunchKernelGGL((sum_kernel<T>), dim3((a.chunks + kSumWaves - 1) / kSumWaves, a.batch), dim3(kSumWaves * 64), 0, st,
+                       a, r);
+  hipLaunchKernelGGL((draw_kernel<T>), dim3(a.batch), dim3(kThreads), 0, st, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t tree_verify_bytes(int, int, int) { return 0; }
+size_t tree_verify_bytes(int batch, int n, int vocab) { return plan_verify(batch, n, vocab, false).bytes; }
 
 hipError_t launch_tree_verify(int batch, int n, int vocab, int dtype, const int32_t* tokens, const int32_t* parent,
                               const void* target, const void* draft, const float* u, const int32_t* counts,
-                              int32_t* path, int32_t* n_path, int32_t* next, void*, hipStream_t st) {
-  const VerifyArgs a = {n, vocab, tokens, parent, static_cast<const char*>(target), static_cast<const char*>(draft), u,
-                        counts, path, n_path, next};
-  if (dtype == SELKV_BF16) hipLaunchKernelGGL((verify_kernel<bf16_t>), dim3(batch), dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((verify_kernel<float>), dim3(batch), dim3(kThreads), 0, st, a);
-  return hipGetLastError();
+                              int32_t* path, int32_t* n_path, int32_t* next, void* ws, hipStream_t st) {
+  const VerifyPlan p = plan_verify(batch, n, vocab, !parent || !draft);
+  char* w = static_cast<char*>(ws);
+  const VerifyArgs a = {n, vocab, p.chunks, tokens, parent, static_cast<const char*>(target),
+                        static_cast<const char*>(draft), u, counts, path, n_path, next, reinterpret_cast<Walk*>(w),
+                        reinterpret_cast<double*>(w + p.parts_off), reinterpret_cast<float2*>(w + p.probs_off), batch,
+                        p.launches};
+  return dtype == SELKV_BF16 ? launch_t<bf16_t>(a, st) : launch_t<float>(a, st);
 }
 
 }  // namespace selkv
