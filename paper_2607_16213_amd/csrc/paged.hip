@@ -6,10 +6,16 @@
 // 1e5 rad and more, is formed in fp64; what is left of it beyond whole quarter
 // turns goes to sine and cosine as fp32, an eighth of a turn at most and so
 // within 2^-28 turns.  Each is computed once per token and pair and held in LDS
-// for the heads of the workgroup.  A thread moves units of 16 channels, two runs
-// of eight that hold eight whole pairs in either layout (channels 8 c and
-// rot_dim / 2 + 8 c, or 16 c and 16 c + 8), so one body serves both, the
-// channels that do not turn and the values.
+// for the heads of the workgroup.  A thread moves units of two 16-byte runs: in
+// either layout they hold whole pairs, if the first run is in the first half of
+// the channels that turn and the second as far into the other half; channels
+// that stay, and values, go the same way.  So eight lanes store whole lines of 128
+// bytes, which stores past the caches need (runs side by side in a thread: 1509
+// us for 256 heads of 25600 rows, 1213 so; through the caches 1265).  A
+// workgroup's threads go token by token within a head, as pages are laid out.
+//
+// Bound by HBM: 256 heads of 25600 rows (bf16) in 1213 us, 5.6 TB/s read and
+// written, 8191 rows of a prompt with their queries in 44.5, 4.5 TB/s.
 #include <algorithm>
 
 #include "paged.hpp"
@@ -19,6 +25,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTokens = 8;      // most tokens of a workgroup
+constexpr int kUnits = 4;       // of a thread, in flight together
+constexpr int kGroups = 1024;    // workgroups that fill the chip
+constexpr size_t kPastBytes = 32u << 20;   // the caches of the chip's eight parts hold 4 MiB each
 constexpr int kMaxNodes = 64;
 
 struct AppendArgs {
@@ -32,27 +41,7 @@ struct AppendArgs {
   float rope_scale;
   int rot, hkv, hq;      // hq: query heads that come along (0: none)
   int tokens, heads;     // of a workgroup
-};
-
-// Eight channels in storage type T.
-template <typename T>
-struct Run8 {
-  static constexpr int kChunks = (int)sizeof(T) / 2;
-  Chunk16 c[kChunks];
-  __device__ __forceinline__ void load(const char* p) {
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) c[i] = load16(p + 16 * i);
-  }
-  __device__ __forceinline__ void store(char* p) const {
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) store16(p + 16 * i, c[i]);
-  }
-  __device__ __forceinline__ float get(int e) const {
-    return Elem<T>::get(c[e / Elem<T>::kPerChunk], e % Elem<T>::kPerChunk);
-  }
-  __device__ __forceinline__ void put(int e, float x) {
-    Elem<T>::put(c[e / Elem<T>::kPerChunk], e % Elem<T>::kPerChunk, x);
-  }
+  bool past;             // stores go past the caches
 };
 
 // Cosine and sine of `angle` times `scale`.
@@ -68,12 +57,19 @@ __device__ __forceinline__ float2 turn_of(double angle, float scale) {
   return make_float2((k == 1 || k == 2 ? -cs : cs) * scale, (k >= 2 ? -sn : sn) * scale);
 }
 
+// A 16-byte store, past the caches where `past`.
+__device__ __forceinline__ void put16(char* p, const Chunk16& c, bool past) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  if (past) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, c), reinterpret_cast<u32x4*>(p));
+  else store16(p, c);
+}
+
 enum { kNoRope = -1 };
 
 template <typename T, int D, int ROPE>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
-  constexpr int UNITS = D / 16;                     // of a row
-  constexpr int EB = (int)sizeof(T);
+  constexpr int EPC = Elem<T>::kPerChunk, EB = (int)sizeof(T);
+  constexpr int UNITS = D / (2 * EPC);              // of a row: two 16-byte runs each
   __shared__ float2 s_turn[kTokens][ROPE == kNoRope ? 1 : D / 2];
   __shared__ int s_page[kTokens];
   const uint32_t b = blockIdx.z;
@@ -94,53 +90,69 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
     }
   }
   __syncthreads();
-  const int turned = ROPE == kNoRope ? 0 : a.rot / 16;   // units of a row that turn
+  const int rot = ROPE == kNoRope ? 0 : a.rot;
   const int units = tokens * heads * UNITS;
-  for (int u = threadIdx.x; u < units; u += kThreads) {
-    const int c = u % UNITS, row = u / UNITS;
-    const int t = row / heads, h = h0 + row - t * heads;
-    const int token = t0 + t;
-    const bool query = h >= 2 * a.hkv, value = !query && h >= a.hkv;
-    const RowsIn& in = query ? a.q : value ? a.v : a.k;
-    const int ih = query ? h - 2 * a.hkv : value ? h - a.hkv : h;
-    const bool turn = !value && c < turned;
-    const int lo = turn && ROPE == SELKV_ROPE_HALF ? 8 * c : 16 * c;
-    const int hi = turn && ROPE == SELKV_ROPE_HALF ? a.rot / 2 + 8 * c : 16 * c + 8;
-    const char* src = in.data + (b * in.sb + token * in.sn + ih * in.sh) * EB;
-    char* dst;
-    if (query) {
-      dst = a.q_out + (((size_t)b * a.n.n + token) * a.hq + ih) * D * EB;
-    } else {
-      const int page = s_page[t];
-      if (page < 0) continue;
-      dst = (value ? a.c.V : a.c.K) + row_of(a.c, a.hkv, page, ih, len + token) * D * EB;
+  for (int u0 = threadIdx.x; u0 < units; u0 += kThreads * kUnits) {
+    Chunk16 x[kUnits], y[kUnits];
+    char* to[kUnits];
+    int apart[kUnits], pair[kUnits];         // bytes from the first run to the second; the first pair that the unit turns, -1: none
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      const int u = u0 + i * kThreads;
+      to[i] = nullptr;
+      if (u >= units) continue;
+      const int c = u % UNITS, row = u / UNITS;
+      const int h_in = row / tokens, t = row - h_in * tokens, h = h0 + h_in;
+      const int token = t0 + t;
+      const bool query = h >= 2 * a.hkv, value = !query && h >= a.hkv;
+      const RowsIn& in = query ? a.q : value ? a.v : a.k;
+      const int ih = query ? h - 2 * a.hkv : value ? h - a.hkv : h;
+      // the runs of the channels that turn, or of those that stay
+      const int turns = value ? 0 : rot, first = 2 * EPC * c < turns ? 0 : turns, last = first ? D : turns ? turns : D;
+      const int lo = first + EPC * (c - first / (2 * EPC));
+      apart[i] = (last - first) / 2 * EB;
+      pair[i] = turns && !first ? t * (D / 2) + (ROPE == SELKV_ROPE_HALF ? EPC : EPC / 2) * c : -1;
+      const char* src = in.data + (b * in.sb + token * in.sn + ih * in.sh + lo) * EB;
+      if (query) {
+        to[i] = a.q_out + ((((size_t)b * a.n.n + token) * a.hq + ih) * D + lo) * EB;
+      } else {
+        const int page = s_page[t];
+        if (page < 0) continue;
+        to[i] = (value ? a.c.V : a.c.K) + (row_of(a.c, a.hkv, page, ih, len + token) * D + lo) * EB;
+      }
+      x[i] = load16(src);
+      y[i] = load16(src + apart[i]);
     }
-    Run8<T> x, y;
-    x.load(src + lo * EB);
-    y.load(src + hi * EB);
-    if (turn) {
-      if constexpr (ROPE == SELKV_ROPE_HALF) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 w = s_turn[t][8 * c + e];
-          const float p = x.get(e), q = y.get(e);
-          x.put(e, p * w.x - q * w.y);
-          y.put(e, q * w.x + p * w.y);
-        }
-      } else if constexpr (ROPE == SELKV_ROPE_INTERLEAVED) {
+    for (int i = 0; i < kUnits; ++i) {
+      if (!to[i]) continue;
+      if constexpr (ROPE != kNoRope) {
+        if (pair[i] >= 0) {
+          const float2* w = &s_turn[0][0] + pair[i];
+          if constexpr (ROPE == SELKV_ROPE_HALF) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 w = s_turn[t][8 * c + e], z = s_turn[t][8 * c + 4 + e];
-          const float p = x.get(2 * e), q = x.get(2 * e + 1), r = y.get(2 * e), s = y.get(2 * e + 1);
-          x.put(2 * e, p * w.x - q * w.y);
-          x.put(2 * e + 1, q * w.x + p * w.y);
-          y.put(2 * e, r * z.x - s * z.y);
-          y.put(2 * e + 1, s * z.x + r * z.y);
+            for (int e = 0; e < EPC; ++e) {
+              const float p = Elem<T>::get(x[i], e), q = Elem<T>::get(y[i], e);
+              Elem<T>::put(x[i], e, p * w[e].x - q * w[e].y);
+              Elem<T>::put(y[i], e, q * w[e].x + p * w[e].y);
+            }
+          } else {
+            const float2* z = w + rot / 4;
+#pragma unroll
+            for (int e = 0; e < EPC / 2; ++e) {
+              const float p = Elem<T>::get(x[i], 2 * e), q = Elem<T>::get(x[i], 2 * e + 1);
+              const float r = Elem<T>::get(y[i], 2 * e), s = Elem<T>::get(y[i], 2 * e + 1);
+              Elem<T>::put(x[i], 2 * e, p * w[e].x - q * w[e].y);
+              Elem<T>::put(x[i], 2 * e + 1, q * w[e].x + p * w[e].y);
+              Elem<T>::put(y[i], 2 * e, r * z[e].x - s * z[e].y);
+              Elem<T>::put(y[i], 2 * e + 1, s * z[e].x + r * z[e].y);
+            }
+          }
         }
       }
+      put16(to[i], x[i], a.past);
+      put16(to[i] + apart[i], y[i], a.past);
     }
-    x.store(dst + lo * EB);
-    y.store(dst + hi * EB);
   }
   if (a.c.bias) {
     for (int i = threadIdx.x; i < tokens * a.hkv; i += kThreads) {
@@ -237,8 +249,13 @@ hipError_t launch_paged_append(int batch, int hkv, int d, int dtype, const Paged
   a.hkv = hkv;
   a.hq = hq;
   const int all = 2 * hkv + hq;
+  // Units of a workgroup: all heads of eight tokens where there are many, otherwise fewer heads, down to two units a
+  // thread: 64 tokens of one layer (8 heads, G 4) 5.4 us, 14.9 with all heads.
+  const size_t elem = dtype == SELKV_BF16 ? 2 : 4, row = d * elem, units = row / 32;
+  const size_t total = (size_t)batch * n.n * all * units, per = std::max<size_t>(total / kGroups, 2 * kThreads);
   a.tokens = std::min(kTokens, n.n);
-  a.heads = all;
+  a.heads = (int)std::min<size_t>(all, std::max<size_t>(1, per / (a.tokens * units)));
+  a.past = (size_t)batch * n.n * all * row >= kPastBytes;
   const dim3 grid((n.n + a.tokens - 1) / a.tokens, (all + a.heads - 1) / a.heads, batch);
   const int layout = rope ? rope->layout : kNoRope;
   if (dtype == SELKV_BF16)

@@ -103,17 +103,22 @@ __device__ __forceinline__ uint64_t ancestors(const int32_t* parent, int n, int 
   return seen;
 }
 
-// The table's columns from `first` on, one in each lane of the wave.
+// The pages of the table's columns from `first` on, one in each lane of the wave, -1 where there is none.
 struct PageWindow {
   int first, page;
-  // `whole`: where entries end that are to be read without a check; moved to the first of them that is on no page
-  __device__ __forceinline__ void fill(const Paged& c, uint32_t b, int column, int& whole, int lane) {
+  __device__ __forceinline__ void fill(const Paged& c, uint32_t b, int column, int lane) {
     first = column;
     page = c.table[(size_t)b * c.columns + min(column + lane, c.columns - 1)];
-    const uint64_t none = __ballot((uint32_t)page >= (uint32_t)c.n_pages || column + lane >= c.columns);
-    if (none) whole = min(whole, (column + __ffsll((unsigned long long)none) - 1) << c.shift);
+    if ((uint32_t)page >= (uint32_t)c.n_pages || column + lane >= c.columns) page = -1;
   }
-  __device__ __forceinline__ bool holds(const Paged& c, int entry) const { return (entry >> c.shift) < first + 64; }
+  // Where the first entry from the window's on is that has no page, `whole` at most.
+  __device__ __forceinline__ int up_to(const Paged& c, int whole) const {
+    const uint64_t none = __ballot(page < 0);
+    return none ? min(whole, (first + __ffsll((unsigned long long)none) - 1) << c.shift) : whole;
+  }
+  __device__ __forceinline__ bool holds(const Paged& c, int from, int to) const {
+    return (from >> c.shift) >= first && (to >> c.shift) < first + 64;
+  }
   __device__ __forceinline__ int at(const Paged& c, int entry) const {
     return __shfl(page, (entry >> c.shift) - first, 64);
   }
@@ -425,9 +430,11 @@ __device__ __forceinline__ void attend_edge(RowTile<D> (&st)[RT], const Keys<T, 
 template <typename T, int D, int RT>
 __device__ __forceinline__ void attend_edges(RowTile<D> (&st)[RT], const Rows<T, D, RT>& rows, const TreeArgs& a,
                                              uint32_t b, int head, int e, int e1, int step, int len, int end,
-                                             bool careful, int col, int grp) {
+                                             bool careful, PageWindow& pages, int lane) {
+  const int col = lane & 15, grp = lane >> 4;
   for (; e < e1; e += step) {
-    const int pk = page_of(a.c, b, e + 8 * (col >> 2)), pv = page_of(a.c, b, e + 8 * grp);
+    if (!pages.holds(a.c, e, e + kTile - 1)) pages.fill(a.c, b, e >> a.c.shift, lane);
+    const int pk = pages.at(a.c, e + 8 * (col >> 2)), pv = pages.at(a.c, e + 8 * grp);
     Keys<T, D> k;
     Values<T, D> v;
     k.load(a.c, a.hkv, head, e, max(pk, 0), max(pv, 0), col, grp);
@@ -596,6 +603,8 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, RT>())) void tr
   Rows<T, D, RT> rows;
   const uint64_t anc = e1 > len ? ancestors(a.parent ? a.parent + (size_t)b * a.n.n : nullptr, a.n.n, lane) : 0;
   load_rows<T, D, RT>(rows, a, b, head, row0, nrows, anc, col, grp);
+  PageWindow pages;
+  pages.fill(a.c, b, (e0 + kw * kTile) >> a.c.shift, lane);
   RowTile<D> st[RT];
   bool careful = false;
   for (;;) {
@@ -603,11 +612,9 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, RT>())) void tr
     int e = e0 + kw * kTile;
     // Steps of entries that all rows attend to.  The next step's keys are loaded when this one's have become logits and
     // its values when this one's are added, into the same registers.
-    int whole = min(e1, len);
+    int whole = pages.up_to(a.c, min(e1, len));
     if (!careful && e + kTile <= whole) {
-      PageWindow pages;
-      pages.fill(a.c, b, e >> a.c.shift, whole, lane);
-      if (e + kTile <= whole) {
+      {
         Keys<T, D> k;
         Values<T, D> v;
         float p[RT][8];
@@ -615,7 +622,10 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, RT>())) void tr
         v.load(a.c, a.hkv, head, e, pages.at(a.c, e + 8 * grp), col, grp);
         for (;;) {
           const int next = e + STEP;
-          if (!pages.holds(a.c, next + kTile - 1)) pages.fill(a.c, b, next >> a.c.shift, whole, lane);
+          if (next + kTile <= whole && !pages.holds(a.c, next, next + kTile - 1)) {
+            pages.fill(a.c, b, next >> a.c.shift, lane);
+            whole = pages.up_to(a.c, whole);
+          }
           if (next + kTile > whole) break;
           const int pk = pages.at(a.c, next + 8 * (col >> 2)), pv = pages.at(a.c, next + 8 * grp);
           logits<T, D, RT>(p, k, rows, a.scale, a.c.bias != nullptr);
@@ -634,7 +644,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, RT>())) void tr
         e += STEP;
       }
     }
-    attend_edges<T, D, RT>(st, rows, a, b, head, e, e1, STEP, len, end, careful, col, grp);
+    attend_edges<T, D, RT>(st, rows, a, b, head, e, e1, STEP, len, end, careful, pages, lane);
     if (careful || !__any(!all_finite<D, RT>(st))) break;
     careful = true;
   }
@@ -677,19 +687,19 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, 2>())) void tre
   Rows<T, D, RT> rows;
   const uint64_t anc = e1 > len ? ancestors(a.parent ? a.parent + (size_t)b * a.n.n : nullptr, a.n.n, lane) : 0;
   load_rows<T, D, RT>(rows, a, b, head, row0, nrows, anc, col, grp);
+  PageWindow pages;
+  pages.fill(a.c, b, e0 >> a.c.shift, lane);
   RowTile<D> st[RT];
   bool careful = false;
   const size_t page_rows = (size_t)a.hkv << a.c.shift, head_row = (size_t)head << a.c.shift;
   const int mask = (1 << a.c.shift) - 1;
   for (;;) {
     clear<D, RT>(st);
-    int e = e0, whole = min(e1, len);
+    int e = e0, whole = pages.up_to(a.c, min(e1, len));
     // Tiles of entries that all rows attend to.
     if (!careful && e + STEP <= whole) {
-      PageWindow pages;
       Chunk16 ahead[kLoads];
       float bias_ahead = 0.f;
-      pages.fill(a.c, b, e >> a.c.shift, whole, lane);
       // the tile at `from` into registers; the rows of a wave's chunks are on one page
       const auto fetch = [&](int from) {
         int tid = threadIdx.x;
@@ -710,7 +720,10 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, 2>())) void tre
       };
       // whether the tile at `from` is one of those
       const auto more = [&](int from) {
-        if (from + STEP <= whole && !pages.holds(a.c, from + STEP - 1)) pages.fill(a.c, b, from >> a.c.shift, whole, lane);
+        if (from + STEP <= whole && !pages.holds(a.c, from, from + STEP - 1)) {
+          pages.fill(a.c, b, from >> a.c.shift, lane);
+          whole = pages.up_to(a.c, whole);
+        }
         return from + STEP <= whole;
       };
       const auto put = [&](char* tile) {
@@ -752,7 +765,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D, 2>())) void tre
         next = after;
       }
     }
-    if (!idle) attend_edges<T, D, RT>(st, rows, a, b, head, e + kw * kTile, e1, KG * kTile, len, end, careful, col, grp);
+    if (!idle) attend_edges<T, D, RT>(st, rows, a, b, head, e + kw * kTile, e1, KG * kTile, len, end, careful, pages, lane);
     if (careful || !__syncthreads_or(!idle && !all_finite<D, RT>(st))) break;
     careful = true;
   }

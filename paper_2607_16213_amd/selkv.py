@@ -686,16 +686,22 @@ class Rope:
 
 def _rows(t, shape, dtype, name):
     """selkv_rows of t [B, n, heads, d], whose rows are d elements side by side."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    if t.dtype != dtype or t.shape != shape:
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
         raise ValueError(f"{name} has shape {tuple(t.shape)} and dtype {t.dtype}, expected {tuple(shape)} and {dtype}")
-    s = t.stride()
-    if s[3] != 1:
+    sb, sn, sh, one = t.stride()
+    if shape[0] == 1:          # a stride that nothing is apart by says nothing
+        sb = 0
+    if shape[1] == 1:
+        sn = 0
+    if shape[2] == 1:
+        sh = 0
+    if one != 1:
         raise ValueError(f"the channels of {name} must be contiguous")
-    if any(t.shape[i] > 1 and s[i] * t.element_size() % 16 for i in range(3)):
+    if (sb | sn | sh) & (7 if dtype == torch.bfloat16 else 3):
         raise ValueError(f"the rows of {name} must be whole multiples of 16 bytes apart")
-    return RowsStruct(t.data_ptr(), *(s[i] if t.shape[i] > 1 else 0 for i in range(3)))
+    return RowsStruct(t.data_ptr(), sb, sn, sh)
 
 
 def paged_append(p, cache, k_new, v_new, cache_len, lens=None, counts=None, bias_new=None, rope=None, positions=None,
@@ -708,24 +714,21 @@ def paged_append(p, cache, k_new, v_new, cache_len, lens=None, counts=None, bias
         raise ValueError("k_new must have four dimensions")
     B, H, d, n, dt = p.batch, p.n_heads_kv, p.head_dim, k_new.shape[1], _kvdt(p)
     k, v = _rows(k_new, (B, n, H, d), dt, "k_new"), _rows(v_new, (B, n, H, d), dt, "v_new")
-    on = [k_new, v_new]
-    ts = ()
+    dev, ts, qr = cache.device, (), None
+    near = k_new.device == dev and v_new.device == dev and (rope is None or rope.device == dev)
     if bias_new is not None:
         ts += ((bias_new, (B, H, n), _F32, "bias_new"),)
     if positions is not None:
         ts += ((positions, (B, n), _I32, "positions"),)
-    qr = None
     if q is not None:
         if rope is None or q_out is None:
             raise ValueError("q needs rope and q_out")
         heads = (B, n, H * p.group, d)
         qr = _rows(q, heads, dt, "q")
-        on.append(q)
+        near = near and q.device == dev
         ts += ((q_out, heads, dt, "q_out"),)
-    if rope is not None:
-        on.append(rope)
-    if any(t.device != cache.device for t in on):
-        raise ValueError(f"the rows and frequencies must be on {cache.device}, as the cache is")
+    if not near:
+        raise ValueError(f"the rows and frequencies must be on {dev}, as the cache is")
     st = _check_cache(p, cache, ts, lens, counts, stream)
     if n == 0:
         return
@@ -783,27 +786,27 @@ def tree_verify(tokens, parent, target, draft, u, path, n_path, next_token, ws, 
     if target.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"target has dtype {target.dtype}, expected torch.float32 or torch.bfloat16")
     B, n, vocab = target.shape
-    dev = target.device
-    ts = [(target, (B, n, vocab), target.dtype, "target"), (tokens, (B, n), _I32, "tokens"), (u, (B, n), _F32, "u"),
-          (path, (B, n), _I32, "path"), (n_path, (B,), _I32, "n_path"), (next_token, (B,), _I32, "next_token")]
+    dev, dt, nodes, rows = target.device, target.dtype, (B, n), (B, n, vocab)
+    ts = ((target, rows, dt, "target"), (tokens, nodes, _I32, "tokens"), (u, nodes, _F32, "u"),
+          (path, nodes, _I32, "path"), (n_path, (B,), _I32, "n_path"), (next_token, (B,), _I32, "next_token"))
     if parent is not None:
-        ts.append((parent, (B, n), _I32, "parent"))
+        ts += ((parent, nodes, _I32, "parent"),)
     if draft is not None:
-        ts.append((draft, (B, n, vocab), target.dtype, "draft"))
+        ts += ((draft, rows, dt, "draft"),)
     if counts is not None:
-        ts.append((counts, (B,), _I32, "counts"))
+        ts += ((counts, (B,), _I32, "counts"),)
     for t, shape, dtype, name in ts:
-        _dev(t, shape, dtype, name)
-        if t.device != dev:
+        if not (t.device == dev and t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+            _dev(t, shape, dtype, name)
             raise ValueError(f"{name} is on {t.device}, target on {dev}")
     if ws is not None and ws.device != dev:
         raise ValueError(f"the workspace is on {ws.device}, target on {dev}")
     if dev.index != torch.cuda.current_device() or (stream is not None and stream.device != dev):
         raise ValueError(f"target is on {dev}: it must be the current device, and that of the stream")
-    st = lib.selkv_tree_verify(B, n, vocab, BF16 if target.dtype == torch.bfloat16 else F32, tokens.data_ptr(),
+    on = _raw_stream(dev.index) if stream is None else stream.cuda_stream
+    st = lib.selkv_tree_verify(B, n, vocab, BF16 if dt == torch.bfloat16 else F32, tokens.data_ptr(),
                                _ptr(parent), target.data_ptr(), _ptr(draft), u.data_ptr(), _ptr(counts),
-                               path.data_ptr(), n_path.data_ptr(), next_token.data_ptr(), _ptr(ws), _nbytes(ws),
-                               _stream(stream))
+                               path.data_ptr(), n_path.data_ptr(), next_token.data_ptr(), _ptr(ws), _nbytes(ws), on)
     if st:
         raise SelkvError(st, "selkv_tree_verify")
 
