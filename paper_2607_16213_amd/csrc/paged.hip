@@ -41,7 +41,6 @@ struct AppendArgs {
   float rope_scale;
   int rot, hkv, hq;      // hq: query heads that come along (0: none)
   int tokens, heads;     // of a workgroup
-  bool past;             // stores go past the caches
 };
 
 // Cosine and sine of `angle` times `scale`.
@@ -57,16 +56,17 @@ __device__ __forceinline__ float2 turn_of(double angle, float scale) {
   return make_float2((k == 1 || k == 2 ? -cs : cs) * scale, (k >= 2 ? -sn : sn) * scale);
 }
 
-// A 16-byte store, past the caches where `past`.
-__device__ __forceinline__ void put16(char* p, const Chunk16& c, bool past) {
+// A 16-byte store, past the caches where PAST.
+template <bool PAST>
+__device__ __forceinline__ void put16(char* p, const Chunk16& c) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  if (past) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, c), reinterpret_cast<u32x4*>(p));
+  if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, c), reinterpret_cast<u32x4*>(p));
   else store16(p, c);
 }
 
 enum { kNoRope = -1 };
 
-template <typename T, int D, int ROPE>
+template <typename T, int D, int ROPE, bool PAST>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
   constexpr int EPC = Elem<T>::kPerChunk, EB = (int)sizeof(T);
   constexpr int UNITS = D / (2 * EPC);              // of a row: two 16-byte runs each
@@ -150,8 +150,8 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
           }
         }
       }
-      put16(to[i], x[i], a.past);
-      put16(to[i] + apart[i], y[i], a.past);
+      put16<PAST>(to[i], x[i]);
+      put16<PAST>(to[i] + apart[i], y[i]);
     }
   }
   if (a.c.bias) {
@@ -219,13 +219,16 @@ __global__ __launch_bounds__(kThreads) void paged_keep_kernel(Paged c, Seqs n, c
 }
 
 template <typename T, int D>
-hipError_t launch_append_t(const AppendArgs& a, int layout, dim3 grid, hipStream_t st) {
+hipError_t launch_append_t(const AppendArgs& a, int layout, bool past, dim3 grid, hipStream_t st) {
+  const auto with = [&](auto near, auto far) {
+    hipLaunchKernelGGL(past ? far : near, grid, dim3(kThreads), 0, st, a);
+  };
   if (layout == SELKV_ROPE_HALF)
-    hipLaunchKernelGGL((paged_append_kernel<T, D, SELKV_ROPE_HALF>), grid, dim3(kThreads), 0, st, a);
+    with(paged_append_kernel<T, D, SELKV_ROPE_HALF, false>, paged_append_kernel<T, D, SELKV_ROPE_HALF, true>);
   else if (layout == SELKV_ROPE_INTERLEAVED)
-    hipLaunchKernelGGL((paged_append_kernel<T, D, SELKV_ROPE_INTERLEAVED>), grid, dim3(kThreads), 0, st, a);
+    with(paged_append_kernel<T, D, SELKV_ROPE_INTERLEAVED, false>, paged_append_kernel<T, D, SELKV_ROPE_INTERLEAVED, true>);
   else
-    hipLaunchKernelGGL((paged_append_kernel<T, D, kNoRope>), grid, dim3(kThreads), 0, st, a);
+    with(paged_append_kernel<T, D, kNoRope, false>, paged_append_kernel<T, D, kNoRope, true>);
   return hipGetLastError();
 }
 
@@ -255,12 +258,12 @@ hipError_t launch_paged_append(int batch, int hkv, int d, int dtype, const Paged
   const size_t total = (size_t)batch * n.n * all * units, per = std::max<size_t>(total / kGroups, 2 * kThreads);
   a.tokens = std::min(kTokens, n.n);
   a.heads = (int)std::min<size_t>(all, std::max<size_t>(1, per / (a.tokens * units)));
-  a.past = (size_t)batch * n.n * all * row >= kPastBytes;
+  const bool past = (size_t)batch * n.n * all * row >= kPastBytes;
   const dim3 grid((n.n + a.tokens - 1) / a.tokens, (all + a.heads - 1) / a.heads, batch);
   const int layout = rope ? rope->layout : kNoRope;
   if (dtype == SELKV_BF16)
-    return d == 128 ? launch_append_t<bf16_t, 128>(a, layout, grid, st) : launch_append_t<bf16_t, 64>(a, layout, grid, st);
-  return d == 128 ? launch_append_t<float, 128>(a, layout, grid, st) : launch_append_t<float, 64>(a, layout, grid, st);
+    return d == 128 ? launch_append_t<bf16_t, 128>(a, layout, past, grid, st) : launch_append_t<bf16_t, 64>(a, layout, past, grid, st);
+  return d == 128 ? launch_append_t<float, 128>(a, layout, past, grid, st) : launch_append_t<float, 64>(a, layout, past, grid, st);
 }
 
 hipError_t launch_paged_keep(int batch, int hkv, int d, int dtype, const Paged& c, const Seqs& n, const int32_t* path,

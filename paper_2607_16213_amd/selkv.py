@@ -219,6 +219,8 @@ def _ptr(t):
 # building a torch Stream object per call.  A torch without GPU support has no
 # such entry, and no call here gets as far as asking for a stream.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# The current device's index, asked only where a device tensor has been seen.
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream(stream):
@@ -501,17 +503,18 @@ def _check_cache(p, cache, tensors, lens, counts, stream):
     if cache._of != (p.batch, p.n_heads_kv, p.head_dim, p.kv_dtype):
         raise ValueError(f"the cache was made for (batch, n_heads_kv, head_dim, kv_dtype) = {cache._of}")
     dev = cache.device
-    if dev.index != torch.cuda.current_device() or (stream is not None and stream.device != dev):
+    at = dev.index
+    if at != _current_device() or (stream is not None and stream.device != dev):
         raise ValueError(f"the cache is on {dev}: it must be the current device, and that of the stream")
     if lens is not None:
         tensors += ((lens, (p.batch,), _I32, "lens"),)
     if counts is not None:
         tensors += ((counts, (p.batch,), _I32, "counts"),)
     for t, shape, dtype, name in tensors:
-        if not (t.device == dev and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+        if t.get_device() != at or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
             _dev(t, shape, dtype, name)
             raise ValueError(f"{name} is on {t.device}, the cache on {dev}")
-    return _raw_stream(dev.index) if stream is None else stream.cuda_stream
+    return _raw_stream(at) if stream is None else stream.cuda_stream
 
 
 def cache8_write(p, cache, K_new, V_new, cache_len, lens=None, counts=None, stream=None):
@@ -715,7 +718,8 @@ def paged_append(p, cache, k_new, v_new, cache_len, lens=None, counts=None, bias
     B, H, d, n, dt = p.batch, p.n_heads_kv, p.head_dim, k_new.shape[1], _kvdt(p)
     k, v = _rows(k_new, (B, n, H, d), dt, "k_new"), _rows(v_new, (B, n, H, d), dt, "v_new")
     dev, ts, qr = cache.device, (), None
-    near = k_new.device == dev and v_new.device == dev and (rope is None or rope.device == dev)
+    at = dev.index
+    near = k_new.get_device() == at and v_new.get_device() == at and (rope is None or rope.device == dev)
     if bias_new is not None:
         ts += ((bias_new, (B, H, n), _F32, "bias_new"),)
     if positions is not None:
@@ -725,7 +729,7 @@ def paged_append(p, cache, k_new, v_new, cache_len, lens=None, counts=None, bias
             raise ValueError("q needs rope and q_out")
         heads = (B, n, H * p.group, d)
         qr = _rows(q, heads, dt, "q")
-        near = near and q.device == dev
+        near = near and q.get_device() == at
         ts += ((q_out, heads, dt, "q_out"),)
     if not near:
         raise ValueError(f"the rows and frequencies must be on {dev}, as the cache is")
@@ -787,7 +791,9 @@ def tree_verify(tokens, parent, target, draft, u, path, n_path, next_token, ws, 
         raise ValueError(f"target has dtype {target.dtype}, expected torch.float32 or torch.bfloat16")
     B, n, vocab = target.shape
     dev, dt, nodes, rows = target.device, target.dtype, (B, n), (B, n, vocab)
-    ts = ((target, rows, dt, "target"), (tokens, nodes, _I32, "tokens"), (u, nodes, _F32, "u"),
+    at = target.get_device()
+    _dev(target, rows, dt, "target")
+    ts = ((tokens, nodes, _I32, "tokens"), (u, nodes, _F32, "u"),
           (path, nodes, _I32, "path"), (n_path, (B,), _I32, "n_path"), (next_token, (B,), _I32, "next_token"))
     if parent is not None:
         ts += ((parent, nodes, _I32, "parent"),)
@@ -796,14 +802,14 @@ def tree_verify(tokens, parent, target, draft, u, path, n_path, next_token, ws, 
     if counts is not None:
         ts += ((counts, (B,), _I32, "counts"),)
     for t, shape, dtype, name in ts:
-        if not (t.device == dev and t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+        if t.get_device() != at or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
             _dev(t, shape, dtype, name)
             raise ValueError(f"{name} is on {t.device}, target on {dev}")
     if ws is not None and ws.device != dev:
         raise ValueError(f"the workspace is on {ws.device}, target on {dev}")
-    if dev.index != torch.cuda.current_device() or (stream is not None and stream.device != dev):
+    if at != _current_device() or (stream is not None and stream.device != dev):
         raise ValueError(f"target is on {dev}: it must be the current device, and that of the stream")
-    on = _raw_stream(dev.index) if stream is None else stream.cuda_stream
+    on = _raw_stream(at) if stream is None else stream.cuda_stream
     st = lib.selkv_tree_verify(B, n, vocab, BF16 if dt == torch.bfloat16 else F32, tokens.data_ptr(),
                                _ptr(parent), target.data_ptr(), _ptr(draft), u.data_ptr(), _ptr(counts),
                                path.data_ptr(), n_path.data_ptr(), next_token.data_ptr(), _ptr(ws), _nbytes(ws), on)
