@@ -16,7 +16,8 @@
  * It then runs the fused selkv_merge_bias into fresh buffers and checks that
  * it reproduces the separate merge and bias bit for bit, and keeps the
  * compressed cache in 8 bits: the decode over the codes must equal the decode
- * over the rows that selkv_cache8_read gives back, up to fp32 rounding.
+ * over the rows that selkv_cache8_read gives back, up to fp32 rounding.  So
+ * must the attention of one node over the same cache in pages equal the decode.
  * Exits 0 on success; on failure prints the failing call and its status. */
 #include <stdio.h>
 #include <stdlib.h>
@@ -65,6 +66,25 @@ static void to_file(FILE* f, const void* dev, size_t bytes) {
   free(h);
 }
 
+/* The relative 2-norm, squared, between two device arrays of n floats. */
+static double distance(const float* a, const float* b, size_t n) {
+  const float* dev[2] = {a, b};
+  float* h[2];
+  for (int i = 0; i < 2; ++i) {
+    h[i] = (float*)malloc(n * sizeof(float));
+    if (!h[i]) exit(5);
+    HIP_OK(hipMemcpy(h[i], dev[i], n * sizeof(float), hipMemcpyDeviceToHost));
+  }
+  double off = 0, norm = 0;
+  for (size_t i = 0; i < n; ++i) {
+    off += ((double)h[0][i] - h[1][i]) * ((double)h[0][i] - h[1][i]);
+    norm += (double)h[1][i] * h[1][i];
+  }
+  free(h[0]);
+  free(h[1]);
+  return off / norm;
+}
+
 /* The compressed cache as int8 codes: written, read back, decoded over.  Returns the relative 2-norm, squared, between the
  * decode over the codes and the decode over the rows read back (ws serves the latter), or exits. */
 static double cache8_check(const selkv_params* p, const void* K_out, const void* V_out, const float* bias, size_t m,
@@ -94,22 +114,45 @@ static double cache8_check(const selkv_params* p, const void* K_out, const void*
   SELKV_OK_(selkv_decode8_attn(p, &c, q, bias8, (int32_t)m, NULL, out[0], ws8, need, st));
   SELKV_OK_(selkv_decode_attn(p, q, K8, V8, bias, (int32_t)m, out[1], ws, ws_bytes, st));
   HIP_OK(hipStreamSynchronize(st));
-  float* h[2];
-  for (int i = 0; i < 2; ++i) {
-    h[i] = (float*)malloc(nq * sizeof(float));
-    if (!h[i]) exit(5);
-    HIP_OK(hipMemcpy(h[i], out[i], nq * sizeof(float), hipMemcpyDeviceToHost));
-  }
-  double off = 0, norm = 0;
-  for (size_t i = 0; i < nq; ++i) {
-    off += ((double)h[0][i] - h[1][i]) * ((double)h[0][i] - h[1][i]);
-    norm += (double)h[1][i] * h[1][i];
-  }
+  const double off = distance(out[0], out[1], nq);
   void* bufs[] = {c.K, c.V, c.k_scale, c.v_scale, c.k_tail, c.v_tail, K8, V8, bias8, out[0], out[1], ws8};
   for (size_t i = 0; i < sizeof(bufs) / sizeof(bufs[0]); ++i) HIP_OK(hipFree(bufs[i]));
-  free(h[0]);
-  free(h[1]);
-  return off / norm;
+  return off;
+}
+
+/* The compressed cache in pages, its last entry taken as the one node of a tree: the same attention as a decode over the
+ * m entries.  Returns the relative 2-norm, squared, to that decode's output `out`, or exits. */
+static double paged_check(const selkv_params* p, const void* K_out, const void* V_out, const float* bias, size_t m,
+                          const void* q, const float* out, hipStream_t st) {
+  const size_t B = (size_t)p->batch, H = (size_t)p->n_heads_kv, d = (size_t)p->head_dim, nq = B * H * p->group * d;
+  selkv_paged c;
+  selkv_paged_init(&c);
+  const size_t P = (size_t)c.page, columns = (m + P - 1) / P, pages = B * columns;
+  c.n_pages = (int32_t)pages;
+  c.columns = (int32_t)columns;
+  c.K = dev_alloc(pages * H * P * d * sizeof(float));
+  c.V = dev_alloc(pages * H * P * d * sizeof(float));
+  c.bias = (float*)dev_alloc(pages * H * P * sizeof(float));
+  int32_t* table = (int32_t*)malloc(pages * sizeof(int32_t));
+  if (!table) exit(5);
+  for (size_t i = 0; i < pages; ++i) table[i] = (int32_t)(pages - 1 - i);
+  int32_t* dtable = (int32_t*)dev_alloc(pages * sizeof(int32_t));
+  HIP_OK(hipMemcpy(dtable, table, pages * sizeof(int32_t), hipMemcpyHostToDevice));
+  c.table = dtable;
+  const int64_t sb = (int64_t)(H * m * d), sn = (int64_t)d, sh = (int64_t)(m * d);   /* rows head by head */
+  const selkv_rows k = {K_out, sb, sn, sh}, v = {V_out, sb, sn, sh};
+  float* got = (float*)dev_alloc(nq * sizeof(float));
+  size_t need = 0;
+  SELKV_OK_(selkv_tree_workspace_size(p, &c, 1, &need));
+  void* ws = dev_alloc(need);
+  SELKV_OK_(selkv_paged_append(p, &c, &k, &v, bias, NULL, NULL, NULL, NULL, (int32_t)m, 0, NULL, NULL, st));
+  SELKV_OK_(selkv_tree_attn(p, &c, q, NULL, 1, (int32_t)m - 1, NULL, NULL, got, ws, need, st));
+  HIP_OK(hipStreamSynchronize(st));
+  const double off = distance(got, out, nq);
+  void* bufs[] = {c.K, c.V, c.bias, dtable, got, ws};
+  for (size_t i = 0; i < sizeof(bufs) / sizeof(bufs[0]); ++i) HIP_OK(hipFree(bufs[i]));
+  free(table);
+  return off;
 }
 
 int main(int argc, char** argv) {
@@ -219,6 +262,12 @@ int main(int argc, char** argv) {
   if (!(off8 < 1e-5 * 1e-5)) {
     fprintf(stderr, "the decode over 8-bit codes is %g (squared) off the decode over their values\n", off8);
     return 8;
+  }
+
+  const double off_pages = paged_check(&p, K_out, V_out, bias, m, q, out, st);
+  if (!(off_pages < 1e-5 * 1e-5)) {
+    fprintf(stderr, "the attention over pages is %g (squared) off the decode over rows\n", off_pages);
+    return 9;
   }
 
   FILE* o = fopen(argv[2], "wb");
