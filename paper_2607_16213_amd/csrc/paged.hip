@@ -70,7 +70,8 @@ template <typename T, int D, int ROPE, bool PAST>
 __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
   constexpr int EPC = Elem<T>::kPerChunk, EB = (int)sizeof(T);
   constexpr int UNITS = D / (2 * EPC);              // of a row: two 16-byte runs each
-  __shared__ float2 s_turn[kTokens][ROPE == kNoRope ? 1 : D / 2];
+  // a token's turns: of a unit's pairs two side by side, then those of the next unit, so that lanes read without conflicts
+  __shared__ __align__(16) float2 s_turn[kTokens][ROPE == kNoRope ? 2 : D / 2];
   __shared__ int s_page[kTokens];
   const uint32_t b = blockIdx.z;
   int len, count;
@@ -86,7 +87,9 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
     for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
       const int t = i / pairs, j = i - t * pairs;
       const int pos = a.positions ? a.positions[(size_t)b * a.n.n + t0 + t] : len + t0 + t;
-      s_turn[t][j] = turn_of((double)pos * a.freq[j], a.rope_scale);
+      constexpr int W = ROPE == SELKV_ROPE_HALF ? EPC : EPC / 2;    // pairs of a unit's run
+      const int run = ROPE == SELKV_ROPE_HALF || j < pairs / 2 ? 0 : pairs / 2, c = (j - run) / W, e = (j - run) % W;
+      s_turn[t][run + ((e >> 1) * (a.rot / (2 * EPC)) + c) * 2 + (e & 1)] = turn_of((double)pos * a.freq[j], a.rope_scale);
     }
   }
   __syncthreads();
@@ -95,7 +98,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
   for (int u0 = threadIdx.x; u0 < units; u0 += kThreads * kUnits) {
     Chunk16 x[kUnits], y[kUnits];
     char* to[kUnits];
-    int apart[kUnits], pair[kUnits];         // bytes from the first run to the second; the first pair that the unit turns, -1: none
+    int apart[kUnits], pair[kUnits];   // bytes from the first run to the second; the place of the unit's turns, -1: none
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const int u = u0 + i * kThreads;
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
       const int turns = value ? 0 : rot, first = 2 * EPC * c < turns ? 0 : turns, last = first ? D : turns ? turns : D;
       const int lo = first + EPC * (c - first / (2 * EPC));
       apart[i] = (last - first) / 2 * EB;
-      pair[i] = turns && !first ? t * (D / 2) + (ROPE == SELKV_ROPE_HALF ? EPC : EPC / 2) * c : -1;
+      pair[i] = turns && !first ? t * (D / 2) + 2 * c : -1;
       const char* src = in.data + (b * in.sb + token * in.sn + ih * in.sh + lo) * EB;
       if (query) {
         to[i] = a.q_out + ((((size_t)b * a.n.n + token) * a.hq + ih) * D + lo) * EB;
@@ -129,23 +132,29 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
       if constexpr (ROPE != kNoRope) {
         if (pair[i] >= 0) {
           const float2* w = &s_turn[0][0] + pair[i];
+          const int next = rot / EPC;           // to the unit's next two
           if constexpr (ROPE == SELKV_ROPE_HALF) {
 #pragma unroll
             for (int e = 0; e < EPC; ++e) {
+              const float4 f = *reinterpret_cast<const float4*>(w + (e >> 1) * next);
+              const float2 r = e & 1 ? make_float2(f.z, f.w) : make_float2(f.x, f.y);
               const float p = Elem<T>::get(x[i], e), q = Elem<T>::get(y[i], e);
-              Elem<T>::put(x[i], e, p * w[e].x - q * w[e].y);
-              Elem<T>::put(y[i], e, q * w[e].x + p * w[e].y);
+              Elem<T>::put(x[i], e, p * r.x - q * r.y);
+              Elem<T>::put(y[i], e, q * r.x + p * r.y);
             }
           } else {
-            const float2* z = w + rot / 4;
 #pragma unroll
             for (int e = 0; e < EPC / 2; ++e) {
+              const float4 f = *reinterpret_cast<const float4*>(w + (e >> 1) * next);
+              const float4 g = *reinterpret_cast<const float4*>(w + rot / 4 + (e >> 1) * next);
+              const float2 r = e & 1 ? make_float2(f.z, f.w) : make_float2(f.x, f.y);
+              const float2 s = e & 1 ? make_float2(g.z, g.w) : make_float2(g.x, g.y);
               const float p = Elem<T>::get(x[i], 2 * e), q = Elem<T>::get(x[i], 2 * e + 1);
-              const float r = Elem<T>::get(y[i], 2 * e), s = Elem<T>::get(y[i], 2 * e + 1);
-              Elem<T>::put(x[i], 2 * e, p * w[e].x - q * w[e].y);
-              Elem<T>::put(x[i], 2 * e + 1, q * w[e].x + p * w[e].y);
-              Elem<T>::put(y[i], 2 * e, r * z[e].x - s * z[e].y);
-              Elem<T>::put(y[i], 2 * e + 1, s * z[e].x + r * z[e].y);
+              const float u = Elem<T>::get(y[i], 2 * e), v = Elem<T>::get(y[i], 2 * e + 1);
+              Elem<T>::put(x[i], 2 * e, p * r.x - q * r.y);
+              Elem<T>::put(x[i], 2 * e + 1, q * r.x + p * r.y);
+              Elem<T>::put(y[i], 2 * e, u * s.x - v * s.y);
+              Elem<T>::put(y[i], 2 * e + 1, v * s.x + u * s.y);
             }
           }
         }
