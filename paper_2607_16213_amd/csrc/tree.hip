@@ -175,28 +175,21 @@ struct Values {
   }
 };
 
-// The same from a tile in LDS.  Rows are RB bytes one after the other; 16-byte chunk c of row r is at chunk c ^ swizzle(r),
-// so that the eight rows whose chunks c are read together, 8 a + b with a = 0, 1 and b = 0 .. 3 (or 4 .. 7), are on
-// different banks.
+// The same from a tile in LDS.  Rows are RB bytes one after the other.  Of K, 16-byte chunk c of row r is at chunk
+// c ^ swizzle(r), so that the rows whose chunks c are read together, 8 a + b with a = 0, 1 and b = 0 .. 3, are on
+// different banks; a V row is read as it lies, and with a swizzle conflicts with the row eight further on.
 __device__ __forceinline__ int swizzle(int row) { return (row & 3) | ((row >> 1) & 4); }
 
-// The places of a lane's chunks: only bit 2 of the swizzle meets bits of j and bits 0 and 1 those of s, so few are kept.
+// The places of a lane's chunks: only bit 2 of the swizzle meets bits of j, so few are kept.
 template <typename T, int D>
 struct Places {
   static constexpr int RB = D * (int)sizeof(T);
-  static constexpr int VC = RB / 16 >= 16 ? RB / 256 : 1;   // 16-byte chunks (or half of one) of a lane of a V row
-  int k[2], v[4][VC], bias;
+  int k[2], v, bias;
   __device__ __forceinline__ Places(int col, int grp) {
     const int row = 8 * (col >> 2) + (col & 3);
 #pragma unroll
     for (int j = 0; j < 2; ++j) k[j] = row * RB + (((4 * j + grp) ^ swizzle(row)) << 4);
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int i = 0; i < VC; ++i) {
-        const int chunk = RB / 16 >= 16 ? col * VC + i : col >> 1;
-        v[s][i] = (8 * grp + s) * RB + ((chunk ^ swizzle(8 * grp + s)) << 4) + (RB / 16 >= 16 ? 0 : (col & 1) * 8);
-      }
+    v = 8 * grp * RB + col * (RB / 16);
     bias = 32 * grp;
   }
 };
@@ -220,20 +213,21 @@ template <typename T, int D>
 __device__ __forceinline__ void read_values(Values<T, D>& x, const char* tile, const Places<T, D>& at) {
   constexpr int RB = D * (int)sizeof(T);
 #pragma unroll
-  for (int s = 0; s < 8; ++s)
+  for (int s = 0; s < 8; ++s) {
+    const char* from = tile + at.v + s * RB;
+    if constexpr (RB / 16 >= 16) {
 #pragma unroll
-    for (int i = 0; i < Places<T, D>::VC; ++i) {
-      const char* from = tile + at.v[s & 3][i] + (s >> 2) * 4 * RB;
-      if constexpr (RB / 16 >= 16) {
-        const Chunk16 w = load16(from);
+      for (int i = 0; i < RB / 256; ++i) {
+        const Chunk16 w = load16(from + 16 * i);
 #pragma unroll
         for (int k = 0; k < 4; ++k) x.v[s][4 * i + k] = w.w[k];
-      } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(from);
-        x.v[s][0] = w.x;
-        x.v[s][1] = w.y;
       }
+    } else {
+      const uint2 w = *reinterpret_cast<const uint2*>(from);
+      x.v[s][0] = w.x;
+      x.v[s][1] = w.y;
     }
+  }
 }
 
 // Softmax state of a wave's row tile: lane (column, grp) keeps its row's maximum, the sum over the entries it holds,
@@ -664,7 +658,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_k
 
 // Calls with more than 32 rows a KV head: the waves of a workgroup share the entries in LDS.  A tile is 32 KG entries, K
 // rows, V rows and biases; two of them alternate, the one after the next is on its way in registers.  Every thread
-// moves 16-byte chunks, chunk i of the tile to place i of LDS, so that the swizzle is one of the addresses in memory.
+// moves 16-byte chunks, chunk i of the tile to place i of LDS, so that the swizzle of K is one of the addresses in memory.
 template <typename T, int D, int RG, int KG>
 __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_shared_kernel(TreeArgs a) {
   constexpr int RT = 2;
@@ -720,9 +714,10 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
           const int at = (tid + i * NT) % kHalf, row = at / CH;
           const int first = (wave * 64 + i * NT) % kHalf / CH;
           const int page = __builtin_amdgcn_readlane(pages.page, ((from + first) >> a.c.shift) - pages.first);
-          const char* rows0 = ((wave * 64 + i * NT) / kHalf ? a.c.V : a.c.K) +
+          const bool value = (wave * 64 + i * NT) / kHalf;
+          const char* rows0 = (value ? a.c.V : a.c.K) +
                               ((size_t)page * page_rows + head_row + ((from + first) & mask & ~7)) * RB;
-          ahead[i] = load16(rows0 + (row - (first & ~7)) * RB + ((at % CH ^ swizzle(row)) << 4));
+          ahead[i] = load16(rows0 + (row - (first & ~7)) * RB + ((at % CH ^ (value ? 0 : swizzle(row))) << 4));
         }
         if (a.c.bias && (int)threadIdx.x < STEP) {
           const int page = __shfl(pages.page, ((from + tid) >> a.c.shift) - pages.first, 64);
