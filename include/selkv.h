@@ -663,7 +663,8 @@ SELKV_API selkv_status selkv_tree_verify_workspace_size(int32_t batch, int32_t n
  *      them; n_path [B] int32, their number; next [B] int32, the token after the
  *      last of them (-1 if the target's row holds no positive probability).  A
  *      sequence with counts[b] outside [1, n] gets n_path 0 and -1 elsewhere.
- * Workspace: selkv_tree_verify_workspace_size(); no initialisation is needed. */
+ * Workspace: selkv_tree_verify_workspace_size(); no initialisation is needed.
+ *      Calls that may overlap in time need separate workspaces. */
 SELKV_API selkv_status selkv_tree_verify(int32_t batch, int32_t n, int32_t vocab, int32_t dtype,
                                          const int32_t* tokens, const int32_t* parent, const void* target,
                                          const void* draft, const float* u, const int32_t* counts, int32_t* path,
