@@ -66,6 +66,36 @@ struct TreeArgs {
   float scale;
 };
 
+struct Sequence {
+  uint32_t b;
+  int len, count;    // count 0: it takes no part
+};
+
+// The sequence that comes at `place`: longest first, in groups of 64, so that the last workgroups of a call are short.
+__device__ __forceinline__ Sequence sequence_at(const Seqs& s, uint32_t place, uint32_t batch, int lane) {
+  Sequence q;
+  const uint32_t first = s.lens ? place & ~63u : place;
+  const int n = s.lens ? (int)min(64u, batch - first) : 1;
+  int work = -1, len = 0, count = 0;     // of the lane's sequence
+  if (lane < n) {
+    if (!sequence_of(s, first + lane, len, count)) count = 0;
+    work = count > 0 ? len + count : 0;
+  }
+  int rank = 0;
+  for (int j0 = 0; j0 < n; j0 += 8) {
+#pragma unroll
+    for (int j = j0; j < j0 + 8; ++j) {
+      const int other = __builtin_amdgcn_readlane(work, j);
+      rank += other > work || (other == work && j < lane);
+    }
+  }
+  const int at = __ffsll((unsigned long long)__ballot(lane < n && rank == (int)(place - first))) - 1;
+  q.b = first + at;
+  q.len = __builtin_amdgcn_readlane(len, at);
+  q.count = __builtin_amdgcn_readlane(count, at);
+  return q;
+}
+
 // Head (of all sequences) and place within its `per` of a block.  Blocks go to the eight parts of the chip in turn, and
 // each part has a cache of its own: all blocks of a head are on one part, if the heads divide into eight, so that what
 // the splits write is in the cache from which the combining kernel reads it (16 nodes over 25600 entries 39.0 us, with
@@ -604,13 +634,14 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_k
   __shared__ __align__(16) f32x4 s_o[kSlots][KG > 1 ? RT * (D / 16) : 1][64];
   __shared__ float2 s_ml[kSlots][RT][64];
   const Place place = place_of(blockIdx.x, a.heads, (uint32_t)(a.splits * a.row_blocks));
-  const uint32_t bh = place.head, b = bh / (uint32_t)a.hkv;
-  const int head = bh - b * a.hkv;
+  const uint32_t at = place.head / (uint32_t)a.hkv;
+  const Sequence seq = sequence_at(a.n, at, a.heads / a.hkv, threadIdx.x & 63);
+  const uint32_t b = seq.b;
+  const int len = seq.len, count = seq.count;
+  const int head = place.head - at * a.hkv;
   const int split = place.inner / a.row_blocks, rb = place.inner % a.row_blocks;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
-  int len, count;
-  if (!sequence_of(a.n, b, len, count)) return;
   const int kw = wave % KG, rw = wave / KG;
   const int nrows = count * a.G;
   if (rb * RG * ROWS >= nrows) return;
@@ -693,20 +724,26 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
   constexpr int kLoads = 2 * kHalf / NT;
   static_assert(2 * kHalf % NT == 0 && kHalf % 64 == 0, "whole chunks a thread, K or V a wave");
   constexpr int kTileBytes = 2 * STEP * RB + STEP * 4;
-  constexpr int kSlots = KG > 1 ? RG * KG / 2 : 0;
+  constexpr bool kHalves = KG == 1;                 // then a turn has two tiles
+  static_assert(!kHalves || SUB == 2, "a tile of a turn for each half of the waves");
+  constexpr int kSlots = KG > 1 ? RG * KG / 2 : RG / 2;
   constexpr int kMergeBytes = kSlots * RT * 64 * ((D / 16) * 16 + 8);
   __shared__ __align__(16) char lds[2 * kTileBytes > kMergeBytes ? 2 * kTileBytes : kMergeBytes];
   const Place place = place_of(blockIdx.x, a.heads, (uint32_t)(a.splits * a.row_blocks));
-  const uint32_t bh = place.head, b = bh / (uint32_t)a.hkv;
-  const int head = bh - b * a.hkv;
+  const uint32_t at = place.head / (uint32_t)a.hkv;
+  const Sequence seq = sequence_at(a.n, at, a.heads / a.hkv, threadIdx.x & 63);
+  const uint32_t b = seq.b;
+  const int len = seq.len, count = seq.count;
+  const int head = place.head - at * a.hkv;
   const int split = place.inner / a.row_blocks, rb = place.inner % a.row_blocks;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
-  int len, count;
-  if (!sequence_of(a.n, b, len, count)) return;
-  const int kw = wave % KG, rw = wave / KG;
   const int nrows = count * a.G;
   if (rb * RG * ROWS >= nrows) return;
+  // where half of the waves hold all rows (a sequence with few of the nodes), each half takes one tile of a turn
+  const bool halves = kHalves && nrows - rb * RG * ROWS <= RG / 2 * ROWS;
+  const int key_groups = halves ? 2 : KG;
+  const int kw = wave % key_groups, rw = wave / key_groups;
   const int row0 = (rb * RG + rw) * ROWS;
   const bool idle = row0 >= nrows;                  // loads and waits with the others
   const int end = len + count;
@@ -776,10 +813,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
         if (next) put(lds + (turn ^ 1) * kTileBytes);
         const bool after = next && more(e + 2 * STEP);
         if (after) fetch(e + 2 * STEP);
-        if (!idle) {
-#pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-          const int sub = u * KG + kw;
+        const auto attend = [&](int sub) {
           float p[RT][8];
           Keys<T, D> k;
           read_keys<T, D>(k, tile + sub * kTile * RB, tile + 2 * STEP * RB + sub * kTile * 4, places);
@@ -788,7 +822,9 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
           read_values<T, D>(v, tile + (STEP + sub * kTile) * RB, places);
           soften<sizeof(T) == 2, D, RT>(st, p, false);
           add_values<T, D, RT>(st, v.v, p);
-        }
+        };
+        if (!idle) {
+          for (int u = 0; u < (halves ? 1 : SUB); ++u) attend(u * KG + kw);
         }
         __syncthreads();
         e += STEP;
@@ -799,15 +835,21 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
     if (!idle) {
       Keys<T, D> k;
       Values<T, D> v;
-      attend_edges<T, D, RT>(st, k, v, false, rows, a, b, head, e + kw * kTile, e1, KG * kTile, len, end, careful, pages,
+      attend_edges<T, D, RT>(st, k, v, false, rows, a, b, head, e + kw * kTile, e1, key_groups * kTile, len, end, careful, pages,
                              lane);
     }
     if (careful || !__syncthreads_or(!idle && !all_finite<D, RT>(st))) break;
     careful = true;
   }
   f32x4* s_o = reinterpret_cast<f32x4*>(lds);
-  finish<T, D, RT, RG, KG>(st, s_o, reinterpret_cast<float2*>(s_o + kSlots * RT * (D / 16) * 64), a, b, head, row0, nrows,
-                           split, rw, kw, lane);
+  float2* s_ml = reinterpret_cast<float2*>(s_o + kSlots * RT * (D / 16) * 64);
+  if constexpr (kHalves) {
+    if (halves) {
+      finish<T, D, RT, RG / 2, 2>(st, s_o, s_ml, a, b, head, row0, nrows, split, rw, kw, lane);
+      return;
+    }
+  }
+  finish<T, D, RT, RG, KG>(st, s_o, s_ml, a, b, head, row0, nrows, split, rw, kw, lane);
 }
 
 // Combines the partials of the rows, in slot order.  A unit of d/4 threads takes four channels each of the slots sub,
