@@ -48,10 +48,12 @@ constexpr int kCUs = 256;
 constexpr uint32_t kParts = 8;         // of the chip
 constexpr int kMaxSplit = 256;
 constexpr int kMaxRounds = 4;          // of workgroups, one a CU
-constexpr int kRaggedRounds = 3;
+constexpr int kRaggedRounds = 2;
+constexpr int kFewRowsRounds = 6;      // up to 32 rows
 constexpr int kGroupCost = 160;        // of a workgroup, and of the second kernel, in entries
 constexpr int kCombineCost = 256;
-constexpr int kFewSlots = 8;           // up to which a row is combined by d/4 threads
+constexpr int kFewSlots = 8;           // up to which a row is combined by d/4 threads; from kManyRows rows on always
+constexpr uint32_t kManyRows = 8192;   // (the ragged call of 128 heads and 208 rows in 10 splits 136 us, 157 without)
 
 struct TreeArgs {
   Paged c;
@@ -71,7 +73,8 @@ struct Sequence {
   int len, count;    // count 0: it takes no part
 };
 
-// The sequence that comes at `place`: longest first, in groups of 64, so that the last workgroups of a call are short.
+// The sequence that comes at `place`: longest first, in groups of 64, so that the last workgroups of a call are short
+// (16 sequences of 0 to 8100 entries, 26 nodes, 8 heads, G 8: 130 us, in the caller's order 167).
 __device__ __forceinline__ Sequence sequence_at(const Seqs& s, uint32_t place, uint32_t batch, int lane) {
   Sequence q;
   const uint32_t first = s.lens ? place & ~63u : place;
@@ -740,7 +743,8 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
   const int col = lane & 15, grp = lane >> 4;
   const int nrows = count * a.G;
   if (rb * RG * ROWS >= nrows) return;
-  // where half of the waves hold all rows (a sequence with few of the nodes), each half takes one tile of a turn
+  // where half of the waves hold all rows (a sequence with few of the nodes), each half takes one tile of a turn (the
+  // call above 125 us, without 130)
   const bool halves = kHalves && nrows - rb * RG * ROWS <= RG / 2 * ROWS;
   const int key_groups = halves ? 2 : KG;
   const int kw = wave % key_groups, rw = wave / key_groups;
@@ -954,7 +958,7 @@ hipError_t launch_td(int64_t heads, const TreePlan& plan, const TreeArgs& a, hip
   if (a.splits > 1) {
     const uint32_t per = (uint32_t)a.n.n * a.G;
     constexpr uint32_t kUnits = 256 / (D / 4);
-    if (a.splits <= kFewSlots)
+    if (a.splits <= kFewSlots || (uint32_t)heads * per >= kManyRows)
       hipLaunchKernelGGL((tree_combine_kernel<T, D, 1>), dim3((uint32_t)heads * ((per + kUnits - 1) / kUnits)), dim3(256), 0,
                          st, a);
     else
@@ -975,10 +979,15 @@ size_t parts_bytes(int64_t heads, int splits, int rows, int d, size_t* ml_off) {
 
 namespace {
 
-// Most splits of a head: kMaxRounds rounds of workgroups.
-int most_splits(int64_t units, int entries, int step) {
-  const int64_t rounds = std::max<int64_t>(1, (int64_t)kMaxRounds * kCUs / units);
-  return (int)std::min<int64_t>({rounds, (int64_t)kMaxSplit, ((int64_t)entries + step - 1) / step});
+// Splits of a head for so many rounds of workgroups.
+int splits_for(int rounds, int64_t units, int entries, int step) {
+  const int64_t splits = ((int64_t)rounds * kCUs + units - 1) / units;
+  return (int)std::min<int64_t>({splits, (int64_t)kMaxSplit, ((int64_t)entries + step - 1) / step});
+}
+
+// Most splits of a head.
+int most_splits(const TreePlan& p, int64_t heads, int entries) {
+  return splits_for(p.row_groups == 1 ? kFewRowsRounds : kMaxRounds, heads * p.row_blocks, entries, p.step);
 }
 
 TreePlan plan_rows(int64_t heads, int d, int rows, size_t elem) {
@@ -999,15 +1008,17 @@ TreePlan plan_rows(int64_t heads, int d, int rows, size_t elem) {
 // How the entries are divided.  A CU reads and computes at one rate however many workgroups share it, so a call takes
 // the entries of a workgroup, and what one costs besides, times the workgroups of the fullest CU: one layer of 25605
 // entries (8 heads, 5 nodes) takes 27.6 us in 29 splits, one workgroup on most CUs, and 29.2 in 51, two on some; 64
-// nodes 78 in 31 and 101 in 51.  Where lengths are the device's to know, three rounds: 16 sequences of 0 to 8100
-// entries (26 nodes, 8 heads) take 154 us in 6 splits, 163 in 4 and 196 in 2.
+// nodes 78 in 31 and 101 in 51.  Where lengths are the device's to know, two rounds, and six up to 32 rows, where a
+// workgroup costs less.  Sequences of 0 to 8100 entries, 8 heads: 8 of up to 64 nodes (G 4) take 77 us in two rounds, 92
+// in one and a half and 81 in three; 16 of up to 26 (G 8) 129, 163 and 117; 16 of up to 16 (G 4) 70, 80 and 82; 32 of up
+// to 8 112 in six and 115 in three, 64 of up to one 30 in six and 64 in one and a half.
 TreePlan plan_tree(int64_t heads, int entries, int d, int rows, size_t elem, bool ragged) {
   TreePlan p = plan_rows(heads, d, rows, elem);
   const int64_t units = heads * p.row_blocks;
-  const int most = most_splits(units, entries, p.step);
+  const int most = splits_for(kMaxRounds, units, entries, p.step);
   p.splits = 1;
   if (ragged) {
-    p.splits = (int)std::min<int64_t>(most, std::max<int64_t>(1, (int64_t)kRaggedRounds * kCUs / units));
+    p.splits = splits_for(p.row_groups == 1 ? kFewRowsRounds : kRaggedRounds, units, entries, p.step);
   } else {
     int64_t best = INT64_MAX;
     for (int s = 1; s <= most; ++s) {
@@ -1026,7 +1037,7 @@ size_t tree_workspace_bound(int64_t heads, int capacity, int d, int G, int n, si
   for (int i = 1; i <= n; ++i) {
     const TreePlan p = plan_rows(heads, d, i * G, elem);
     size_t ml_off;
-    most = std::max(most, parts_bytes(heads, most_splits(heads * p.row_blocks, capacity, p.step), i * G, d, &ml_off));
+    most = std::max(most, parts_bytes(heads, most_splits(p, heads, capacity), i * G, d, &ml_off));
   }
   return most;
 }
