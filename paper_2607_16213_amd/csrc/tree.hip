@@ -291,6 +291,7 @@ __device__ __forceinline__ void read_values(Values<T, D>& x, const char* tile, c
 template <int D>
 struct RowTile {
   float m, l;
+  bool far;              // the same in all lanes: a maximum of the wave's is beyond kFar (of its first tile alone)
   f32x4 o[D / 16];
 };
 
@@ -400,10 +401,13 @@ __device__ __forceinline__ void logits(float (&p)[RT][8], const Keys<T, D>& x, c
 constexpr float kSlack = 6.f;
 
 // Logits to weights, with the running maximum and sum.  Before bf16 weights the maximum is taken off by the fma that
-// turns a logit to powers of two (its product with log2(e), rounded once, is the same for all of a row); a maximum
-// beyond 2^127 / log2(e) makes that infinite, and the results NaN: a careful pass takes such a one off by itself.
+// turns a logit to powers of two.  Its product with log2(e) is rounded once, the same for all of a row, so weights are off
+// by one factor: up to |m| = kFar by 2^-14 of themselves at most, as much as a logit's own rounding moves it.  The factor
+// grows with |m| (up to 2^64 at 1e9, out of any range at 1e11), so a row with a maximum beyond kFar has it taken off first.
+constexpr float kFar = 1024.f;
+
 template <bool FUSED, int D, int RT>
-__device__ __forceinline__ void soften(RowTile<D> (&st)[RT], float (&p)[RT][8], bool careful) {
+__device__ __forceinline__ void soften(RowTile<D> (&st)[RT], float (&p)[RT][8]) {
   float top[RT];
   bool above = false;
 #pragma unroll
@@ -424,14 +428,31 @@ __device__ __forceinline__ void soften(RowTile<D> (&st)[RT], float (&p)[RT][8], 
       for (int i = 0; i < D / 16; ++i) st[t].o[i] *= corr;
       st[t].m = m;
     }
+    if (FUSED) {
+      bool far = false;
+#pragma unroll
+      for (int t = 0; t < RT; ++t) far = far || (fabsf(st[t].m) > kFar && st[t].m != kNegInf);
+      st[0].far = __any(far);
+    }
+  }
+  float ref[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) ref[t] = st[t].m == kNegInf ? 0.f : st[t].m;   // nothing unmasked yet: every weight is 0
+  if (FUSED && __builtin_expect(st[0].far, 0)) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const float first = fabsf(ref[t]) > kFar ? ref[t] : 0.f;   // by row here too
+#pragma unroll
+      for (int s = 0; s < 8; ++s) p[t][s] -= first;
+      ref[t] -= first;
+    }
   }
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const float ref = st[t].m == kNegInf ? 0.f : st[t].m;   // nothing unmasked yet: every weight is 0
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      if (FUSED && !(careful && !finite(ref * kLog2e))) p[t][s] = fast_exp2(fmaf(p[t][s], kLog2e, -ref * kLog2e));
-      else p[t][s] = fast_exp2((p[t][s] - ref) * kLog2e);
+      if (FUSED) p[t][s] = fast_exp2(fmaf(p[t][s], kLog2e, -ref[t] * kLog2e));
+      else p[t][s] = fast_exp2((p[t][s] - ref[t]) * kLog2e);
       st[t].l += p[t][s];
     }
   }
@@ -459,7 +480,7 @@ __device__ __forceinline__ void attend_edge(RowTile<D> (&st)[RT], const Keys<T, 
       else if (careful) x.v[s][w] = zero_unbounded<T>(x.v[s][w], unbounded);
     }
   }
-  soften<sizeof(T) == 2, D, RT>(st, p, careful);
+  soften<sizeof(T) == 2, D, RT>(st, p);
   add_values<T, D, RT>(st, x.v, p);
   if (careful && __any(unbounded)) {
     for (int s = 0; s < kTile; ++s) {
@@ -602,6 +623,7 @@ __device__ __forceinline__ void clear(RowTile<D> (&st)[RT]) {
   for (int t = 0; t < RT; ++t) {
     st[t].m = kNegInf;
     st[t].l = 0.f;
+    st[t].far = false;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) st[t].o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -688,7 +710,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_k
           __builtin_amdgcn_sched_barrier(0);   // loads moved up would need registers of their own
           k.load(a.c, a.hkv, head, next, pk, pv, col, grp);
           __builtin_amdgcn_sched_barrier(0);
-          soften<sizeof(T) == 2, D, RT>(st, p, false);
+          soften<sizeof(T) == 2, D, RT>(st, p);
           add_values<T, D, RT>(st, v.v, p);
           __builtin_amdgcn_sched_barrier(0);
           v.load(a.c, a.hkv, head, next, pv, col, grp);
@@ -701,7 +723,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_k
         __builtin_amdgcn_sched_barrier(0);
         if (loaded) k.load(a.c, a.hkv, head, e, pk, pv, col, grp);
         __builtin_amdgcn_sched_barrier(0);
-        soften<sizeof(T) == 2, D, RT>(st, p, false);
+        soften<sizeof(T) == 2, D, RT>(st, p);
         add_values<T, D, RT>(st, v.v, p);
         __builtin_amdgcn_sched_barrier(0);
         if (loaded) v.load(a.c, a.hkv, head, e, pv, col, grp);
@@ -824,7 +846,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
           logits<T, D, RT>(p, k, rows, a.scale, true);
           Values<T, D> v;
           read_values<T, D>(v, tile + (STEP + sub * kTile) * RB, places);
-          soften<sizeof(T) == 2, D, RT>(st, p, false);
+          soften<sizeof(T) == 2, D, RT>(st, p);
           add_values<T, D, RT>(st, v.v, p);
         };
         if (!idle) {
