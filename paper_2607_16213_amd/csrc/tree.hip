@@ -28,11 +28,12 @@
 //
 // Masks.  Entries past the end, on no page or (for a node) outside its chain of
 // parents are left out by selection in the tiles that hold such; a masked bias
-// makes a logit -inf by itself.  Where a result comes out NaN or infinite the
+// makes a logit -inf by itself.  Where a result comes out NaN, infinite or past 2^96 the
 // wave does its entries again in a careful pass, in which every tile selects
 // masked biases too, V's values that are NaN or infinite are kept out of the
 // product, where a weight of 0 would turn them into NaN for every row, and are
-// added to the rows that attend to them.
+// added to the rows that attend to them.  Its weights are a power of two smaller,
+// so that no sum of finite values overflows: a mean of finite values is finite.
 //
 // Split-K: a workgroup takes a run of entries, and a second kernel combines the
 // runs' (max, sum, o) in order.
@@ -400,14 +401,14 @@ __device__ __forceinline__ void logits(float (&p)[RT][8], const Keys<T, D>& x, c
 // 8100 entries, 26 nodes).  Weights are up to e^6 then, which fp32 sums and the weights' relative rounding do not mind.
 constexpr float kSlack = 6.f;
 
-// Logits to weights, with the running maximum and sum.  Before bf16 weights the maximum is taken off by the fma that
+// Logits to weights, with the running maximum and sum; the weights are multiplied by `lower`.  Before bf16 weights the maximum is taken off by the fma that
 // turns a logit to powers of two.  Its product with log2(e) is rounded once, the same for all of a row, so weights are off
 // by one factor: up to |m| = kFar by 2^-14 of themselves at most, as much as a logit's own rounding moves it.  The factor
 // grows with |m| (up to 2^64 at 1e9, out of any range at 1e11), so a row with a maximum beyond kFar has it taken off first.
 constexpr float kFar = 1024.f;
 
 template <bool FUSED, int D, int RT>
-__device__ __forceinline__ void soften(RowTile<D> (&st)[RT], float (&p)[RT][8]) {
+__device__ __forceinline__ void soften(RowTile<D> (&st)[RT], float (&p)[RT][8], float lower) {
   float top[RT];
   bool above = false;
 #pragma unroll
@@ -453,17 +454,19 @@ __device__ __forceinline__ void soften(RowTile<D> (&st)[RT], float (&p)[RT][8]) 
     for (int s = 0; s < 8; ++s) {
       if (FUSED) p[t][s] = fast_exp2(fmaf(p[t][s], kLog2e, -ref[t] * kLog2e));
       else p[t][s] = fast_exp2((p[t][s] - ref[t]) * kLog2e);
+      p[t][s] *= lower;
       st[t].l += p[t][s];
     }
   }
 }
 
 // A step whose 32 entries from `base` may be behind len, the entries that all rows attend to, behind end, the nodes after
-// them, or on no page (pv < 0); or one of a careful pass.
+// them, or on no page (pv < 0); or one of a careful pass, whose weights are `lower` (1 otherwise).
 template <typename T, int D, int RT>
 __device__ __forceinline__ void attend_edge(RowTile<D> (&st)[RT], const Keys<T, D>& k, Values<T, D>& x,
                                             const Rows<T, D, RT>& rows, const TreeArgs& a, uint32_t b, int head, int base,
-                                            int len, int end, int pv, bool careful, int grp) {
+                                            int len, int end, int pv, float lower, int grp) {
+  const bool careful = lower < 1.f;
   float p[RT][8];
   logits<T, D, RT>(p, k, rows, a.scale, a.c.bias != nullptr);
   bool unbounded = false;
@@ -480,7 +483,7 @@ __device__ __forceinline__ void attend_edge(RowTile<D> (&st)[RT], const Keys<T, 
       else if (careful) x.v[s][w] = zero_unbounded<T>(x.v[s][w], unbounded);
     }
   }
-  soften<sizeof(T) == 2, D, RT>(st, p);
+  soften<sizeof(T) == 2, D, RT>(st, p, lower);
   add_values<T, D, RT>(st, x.v, p);
   if (careful && __any(unbounded)) {
     for (int s = 0; s < kTile; ++s) {
@@ -501,7 +504,7 @@ __device__ __forceinline__ void attend_edge(RowTile<D> (&st)[RT], const Keys<T, 
 template <typename T, int D, int RT>
 __device__ __forceinline__ void attend_edges(RowTile<D> (&st)[RT], Keys<T, D>& k, Values<T, D>& v, bool loaded,
                                              const Rows<T, D, RT>& rows, const TreeArgs& a, uint32_t b, int head, int e,
-                                             int e1, int step, int len, int end, bool careful, PageWindow& pages,
+                                             int e1, int step, int len, int end, float lower, PageWindow& pages,
                                              int lane) {
   const int col = lane & 15, grp = lane >> 4;
   for (; e < e1; e += step) {
@@ -512,7 +515,7 @@ __device__ __forceinline__ void attend_edges(RowTile<D> (&st)[RT], Keys<T, D>& k
       v.load(a.c, a.hkv, head, e, max(pv, 0), col, grp);
     }
     loaded = false;
-    attend_edge<T, D, RT>(st, k, v, rows, a, b, head, e, len, end, pv, careful, grp);
+    attend_edge<T, D, RT>(st, k, v, rows, a, b, head, e, len, end, pv, lower, grp);
   }
 }
 
@@ -629,16 +632,47 @@ __device__ __forceinline__ void clear(RowTile<D> (&st)[RT]) {
   }
 }
 
+// Sums up to this are merged as they are: with those of all other waves and splits they stay in range.
+constexpr float kRoom = 0x1p96f;
+
 template <int D, int RT>
-__device__ __forceinline__ bool all_finite(const RowTile<D> (&st)[RT]) {
+__device__ __forceinline__ bool all_in_range(const RowTile<D> (&st)[RT]) {
   bool fine = true;
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) fine = fine && finite(st[t].o[i][r]);
+      for (int r = 0; r < 4; ++r) fine = fine && fabsf(st[t].o[i][r]) < kRoom;
   return fine;
+}
+
+// By which power of two the weights of a careful pass are smaller: `end` of them, up to e^8 each (kSlack, rounded where
+// maxima are large), add up to less than 1.
+__device__ __forceinline__ int careful_shift(int end) { return 44 - __clz(end); }
+
+// After a careful pass: rows whose sums are small get the power of two back, which leaves the bits of a pass that never
+// took it off; the others' maximum is raised by as much.
+template <int D, int RT>
+__device__ __forceinline__ void settle(RowTile<D> (&st)[RT], int shift) {
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, finite(st[t].o[i][r]) ? fabsf(st[t].o[i][r]) : 0.f);
+    top = max_xor32(max_xor16(top));
+    float back = ldexpf(1.f, shift);
+    if (top * back >= kRoom) {
+      const float raised = st[t].m + (float)shift / kLog2e;
+      back = fast_exp2((float)shift - (raised - st[t].m) * kLog2e);   // 1 but for the rounding of `raised`
+      st[t].m = raised;
+    }
+    st[t].l *= back;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) st[t].o[i] *= back;
+  }
 }
 
 // Waves a SIMD is to hold: what the registers of the accumulators, queries and the step on its way leave (one row tile of
@@ -710,7 +744,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_k
           __builtin_amdgcn_sched_barrier(0);   // loads moved up would need registers of their own
           k.load(a.c, a.hkv, head, next, pk, pv, col, grp);
           __builtin_amdgcn_sched_barrier(0);
-          soften<sizeof(T) == 2, D, RT>(st, p);
+          soften<sizeof(T) == 2, D, RT>(st, p, 1.f);
           add_values<T, D, RT>(st, v.v, p);
           __builtin_amdgcn_sched_barrier(0);
           v.load(a.c, a.hkv, head, next, pv, col, grp);
@@ -723,16 +757,18 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_k
         __builtin_amdgcn_sched_barrier(0);
         if (loaded) k.load(a.c, a.hkv, head, e, pk, pv, col, grp);
         __builtin_amdgcn_sched_barrier(0);
-        soften<sizeof(T) == 2, D, RT>(st, p);
+        soften<sizeof(T) == 2, D, RT>(st, p, 1.f);
         add_values<T, D, RT>(st, v.v, p);
         __builtin_amdgcn_sched_barrier(0);
         if (loaded) v.load(a.c, a.hkv, head, e, pv, col, grp);
       }
     }
-    attend_edges<T, D, RT>(st, k, v, loaded, rows, a, b, head, e, e1, STEP, len, end, careful, pages, lane);
-    if (careful || !__any(!all_finite<D, RT>(st))) break;
+    attend_edges<T, D, RT>(st, k, v, loaded, rows, a, b, head, e, e1, STEP, len, end,
+                           careful ? ldexpf(1.f, -careful_shift(end)) : 1.f, pages, lane);
+    if (careful || !__any(!all_in_range<D, RT>(st))) break;
     careful = true;
   }
+  if (careful) settle<D, RT>(st, careful_shift(end));
   finish<T, D, RT, RG, KG>(st, s_o[0][0], s_ml[0][0], a, b, head, row0, nrows, split, rw, kw, lane);
 }
 
@@ -846,7 +882,7 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
           logits<T, D, RT>(p, k, rows, a.scale, true);
           Values<T, D> v;
           read_values<T, D>(v, tile + (STEP + sub * kTile) * RB, places);
-          soften<sizeof(T) == 2, D, RT>(st, p);
+          soften<sizeof(T) == 2, D, RT>(st, p, 1.f);
           add_values<T, D, RT>(st, v.v, p);
         };
         if (!idle) {
@@ -861,12 +897,13 @@ __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_s
     if (!idle) {
       Keys<T, D> k;
       Values<T, D> v;
-      attend_edges<T, D, RT>(st, k, v, false, rows, a, b, head, e + kw * kTile, e1, key_groups * kTile, len, end, careful, pages,
-                             lane);
+      attend_edges<T, D, RT>(st, k, v, false, rows, a, b, head, e + kw * kTile, e1, key_groups * kTile, len, end,
+                             careful ? ldexpf(1.f, -careful_shift(end)) : 1.f, pages, lane);
     }
-    if (careful || !__syncthreads_or(!idle && !all_finite<D, RT>(st))) break;
+    if (careful || !__syncthreads_or(!idle && !all_in_range<D, RT>(st))) break;
     careful = true;
   }
+  if (careful) settle<D, RT>(st, careful_shift(end));
   f32x4* s_o = reinterpret_cast<f32x4*>(lds);
   float2* s_ml = reinterpret_cast<float2*>(s_o + kSlots * RT * (D / 16) * 64);
   if constexpr (kHalves) {

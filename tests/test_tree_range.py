@@ -87,3 +87,42 @@ def test_biases_of_many_sizes(S, dtype, n, G, L, counts):
             _, v, _ = U.entries(c.c, b, at, step)
             mean, size = (np.broadcast_to(np.repeat(x.mean(0), G, 0), (m, 2 * G, 128)) for x in (v, np.abs(v)))
             U.assert_near(U.host(out[b, :m]), mean, size, 0.0, step, dtype, b)
+
+
+def assert_means(c, b, out, note):
+    """Every output against 64 bits.  One entry may be all that counts in a channel, so the error of a single weight does:
+    a logit is a sum of d products, and each of d + 2 roundings is at most 2^-24 of A, the sum of the products'
+    magnitudes and the bias; a weight's error is that of its logit and of the sum of weights, each rounded in an
+    exponential of 2^-22 and, for bf16, in two numbers, 2^-16.  The accumulators' roundings are those of assert_near."""
+    want, size, _, entries = c.want(b)
+    m = c.nodes(b)
+    k, _, bias = U.entries(c.c, b, 0, entries)
+    q, d = np.abs(U.host(c.q[b, :m])), c.q.shape[-1]
+    A = max((q[:, h] @ np.abs(k[:, h // c.G]).T * c.scale).max() for h in range(q.shape[1])) + np.abs(bias).max()
+    rel = 2 * (d + 2) * 2.0 ** -24 * A + 2.0 ** -21 + 2.0 ** -24 * (24 + entries / 4) + (2.0 ** -15 if c.dtype == "bf16" else 0)
+    got = U.host(out[b, :m])
+    assert np.isfinite(got).all(), note
+    tol = rel * size + U.half_step(c.dtype) * np.abs(want) * 1.01
+    assert (np.abs(got - want) <= tol).all(), (note, (np.abs(got - want) / tol).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,G,L,counts", SHAPES)
+@pytest.mark.parametrize("where", ["all", "a few", "one split", "nodes"])
+def test_finite_values_give_finite_means(S, dtype, n, G, L, counts, where):
+    """Values up to 3e38: their weighted mean is finite, so is the output."""
+    for signs, spread in ((False, 1.0), (True, 1.0), (True, 6.0)):
+        c = call(S, dtype, n, G, L, counts, 44, spread=spread)
+        g = U.gen(45)
+        for b in range(len(c.lens)):
+            m = c.nodes(b)
+            first, count = {"all": (0, L + m), "a few": (L // 2, 3), "one split": (0, min(L, 128)), "nodes": (L, m)}[where]
+            pg, row = U.places(c.c, b, first, count)
+            x = 10.0 ** (36.0 + 2.47 * torch.rand((count, 2, 128), generator=g, device=DEV).double())
+            if signs:
+                x *= torch.where(torch.rand(x.shape, generator=g, device=DEV) < 0.5, -1.0, 1.0)
+            c.c.V[pg, :, row] = x.to(c.c.V.dtype)
+        assert bool(torch.isfinite(c.c.V[c.c.table[0, 0].long()]).all())
+        out = c.run()
+        for b in range(len(c.lens)):
+            assert_means(c, b, out, (where, signs, spread, b))
