@@ -123,7 +123,11 @@ __device__ __forceinline__ int chunk_of(const TreeArgs& a, int total) {
   return (int)(max((per + step - 1) / step, 1u) * step);
 }
 
-__device__ __forceinline__ float weight_of(float m, float M) { return m == kNegInf ? 0.f : fast_exp2((m - M) * kLog2e); }
+// What sums with maximum m count for beside M.  One below fp32's range is its smallest number: nothing to finite sums, and
+// infinite ones stay infinite (0 would make them NaN, by where their entries lie; chosen by value 32.6 us where 28.1).
+__device__ __forceinline__ float weight_of(float m, float M) {
+  return m == kNegInf ? 0.f : fmaxf(fast_exp2((m - M) * kLog2e), 0x1p-149f);
+}
 
 // The maximum that goes with a sum: fmaxf passes a NaN logit by, so where the sum is NaN a part keeps a maximum that
 // makes it count.

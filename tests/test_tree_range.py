@@ -126,3 +126,30 @@ def test_finite_values_give_finite_means(S, dtype, n, G, L, counts, where):
         out = c.run()
         for b in range(len(c.lens)):
             assert_means(c, b, out, (where, signs, spread, b))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,G,L,counts", SHAPES)
+def test_infinite_values_with_hardly_a_weight(S, dtype, n, G, L, counts):
+    """e^-200 of infinity is infinite, wherever the entry lies: in a row's first tile or its last, in tiles, waves and
+    splits of such entries alone or beside others."""
+    inf = float("inf")
+    for first, count in ((0, L * 3 // 4), (L // 4, L * 3 // 4), (0, 0)):
+        c = call(S, dtype, n, G, L, counts, 46)
+        for b in range(len(c.lens)):
+            bias_of(c, b, first, count, -200.0)
+        good = c.run()
+        for b in range(len(c.lens)):
+            for j, e in enumerate((0, 5, L // 3, L // 2, L - 1)):
+                pg, row = U.places(c.c, b, e, 1)
+                c.c.V[pg, :, row, 10 + j] = -inf if j % 2 else inf
+                c.c.bias[pg, :, row] = -200.0
+        for b in range(len(c.lens)):
+            bias_of(c, b, 0, 5, -300.0)        # behind which more comes in any case
+        out = c.run()
+        for b in range(len(c.lens)):
+            m = c.nodes(b)
+            for j in range(5):
+                assert bool((out[b, :m, :, 10 + j] == (-inf if j % 2 else inf)).all()), (first, b, j)
+            rest = [j for j in range(128) if not 10 <= j < 15]
+            assert bool(torch.isfinite(out[b, :m][..., rest]).all()) and bool(torch.isfinite(good[b, :m]).all())
