@@ -655,6 +655,7 @@ SELKV_API selkv_status selkv_tree_verify_workspace_size(int32_t batch, int32_t n
  * p, S (1 at first) becomes max(S - p(x), 0), and x refused once is refused again.
  * All of this is fp64 on the probabilities as given.  A weight that is negative
  * or NaN counts as 0 and accepts nothing; a token outside [0, vocab) is refused.
+ * The draft's row of a node without children is not read: it may hold anything.
  * In:  tokens [B, n] int32 (of node 0 it is not read); parent [B, n] int32 or
  *      NULL; target and draft (or NULL) [B, n, vocab] in dtype (selkv_dtype);
  *      u [B, n] fp32 in [0, 1); counts [B] int32 or NULL; 1 <= n <= 64;

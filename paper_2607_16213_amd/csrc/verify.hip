@@ -104,7 +104,7 @@ struct Dist {
   static constexpr int N = Elem<T>::kPerChunk;
   static constexpr int kSteps = kChunk / (64 * N);
   const char* p;       // aligned down
-  const char* q;       // nullptr: no draft
+  const char* q;       // nullptr: nothing of a draft is taken out
   int shift, vocab;
   double c;
   uint64_t out;        // nodes whose tokens are taken out (without a draft)
@@ -321,7 +321,8 @@ struct Walker {
     const size_t at = (node0 + s.at) * row_bytes;
     dist.shift = (int)(at % 16 / sizeof(T));
     dist.p = a->target + at / 16 * 16;
-    dist.q = a->draft ? a->draft + at / 16 * 16 : nullptr;
+    // with nothing taken out the weights are p, whatever q: a row that no child was drawn from may hold anything
+    dist.q = a->draft && s.c != 0.0 ? a->draft + at / 16 * 16 : nullptr;
     dist.c = s.c;
     dist.out = s.out;
   }
