@@ -29,6 +29,7 @@ constexpr int kUnits = 4;       // of a thread, in flight together
 constexpr int kGroups = 1024;    // workgroups that fill the chip
 constexpr size_t kPastBytes = 32u << 20;   // the caches of the chip's eight parts hold 4 MiB each
 constexpr int kMaxNodes = 64;
+constexpr int kMaxLaunchRows = 1 << 26;    // a dimension of a grid has less than 2^32 threads: 2^24 workgroups of kTokens rows
 
 struct AppendArgs {
   Paged c;
@@ -41,6 +42,7 @@ struct AppendArgs {
   float rope_scale;
   int rot, hkv, hq;      // hq: query heads that come along (0: none)
   int tokens, heads;     // of a workgroup
+  int first;             // row of the launch
 };
 
 // Cosine and sine of `angle` times `scale`.
@@ -76,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
   const uint32_t b = blockIdx.z;
   int len, count;
   if (!sequence_of(a.n, b, len, count)) return;
-  const int t0 = blockIdx.x * a.tokens;
+  const int t0 = a.first + blockIdx.x * a.tokens;
   const int tokens = min(a.tokens, count - t0);
   if (tokens <= 0) return;
   const int all = 2 * a.hkv + a.hq;
@@ -269,11 +271,17 @@ hipError_t launch_paged_append(int batch, int hkv, int d, int dtype, const Paged
   a.tokens = std::min(kTokens, n.n);
   a.heads = (int)std::min<size_t>(all, std::max<size_t>(1, per / (a.tokens * units)));
   const bool past = (size_t)batch * n.n * all * row >= kPastBytes;
-  const dim3 grid((n.n + a.tokens - 1) / a.tokens, (all + a.heads - 1) / a.heads, batch);
   const int layout = rope ? rope->layout : kNoRope;
-  if (dtype == SELKV_BF16)
-    return d == 128 ? launch_append_t<bf16_t, 128>(a, layout, past, grid, st) : launch_append_t<bf16_t, 64>(a, layout, past, grid, st);
-  return d == 128 ? launch_append_t<float, 128>(a, layout, past, grid, st) : launch_append_t<float, 64>(a, layout, past, grid, st);
+  hipError_t e = hipSuccess;
+  for (a.first = 0; a.first < n.n && e == hipSuccess; a.first += kMaxLaunchRows) {
+    const int rows = std::min(n.n - a.first, kMaxLaunchRows);
+    const dim3 grid((rows + a.tokens - 1) / a.tokens, (all + a.heads - 1) / a.heads, batch);
+    if (dtype == SELKV_BF16)
+      e = d == 128 ? launch_append_t<bf16_t, 128>(a, layout, past, grid, st) : launch_append_t<bf16_t, 64>(a, layout, past, grid, st);
+    else
+      e = d == 128 ? launch_append_t<float, 128>(a, layout, past, grid, st) : launch_append_t<float, 64>(a, layout, past, grid, st);
+  }
+  return e;
 }
 
 hipError_t launch_paged_keep(int batch, int hkv, int d, int dtype, const Paged& c, const Seqs& n, const int32_t* path,
