@@ -956,7 +956,10 @@ class TreeDecoder:
     def attend(self, q, k_new, v_new, cache_len, parent=None, lens=None, counts=None, rope=None, positions=None,
                stream=None):
         """Append the nodes' rows k_new, v_new [B, n, H, d] and attend with q [B, n, H G, d]; where rope is given, q and
-        k_new are turned by positions [B, n] (cache_len + i without them) first."""
+        k_new are turned by positions [B, n] first.  Without positions node i is at cache_len + i (lens[b] + i), as the
+        nodes of a chain are; siblings share one, so a tree needs them."""
+        if rope is not None and parent is not None and positions is None:
+            raise ValueError("a tree's nodes are at their depth, not in a row: positions are needed with rope and parent")
         out = self._front(self.out, q.shape[1])
         turned = None if rope is None else self._front(self.q, q.shape[1])
         paged_append(self.p, self.cache, k_new, v_new, cache_len, lens, counts, rope=rope, positions=positions,
