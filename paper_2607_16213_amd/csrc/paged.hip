@@ -14,8 +14,9 @@
 // us for 256 heads of 25600 rows, 1213 so; through the caches 1265).  A
 // workgroup's threads go token by token within a head, as pages are laid out.
 //
-// Bound by HBM: 256 heads of 25600 rows (bf16) in 1213 us, 5.6 TB/s read and
-// written, 8191 rows of a prompt with their queries in 39.6, 5.1 TB/s.
+// Bound by HBM: 256 heads of 25600 rows (bf16) in 1213 to 1310 us by the box,
+// 5.2 to 5.6 TB/s read and written, 8191 rows of a prompt with their queries in
+// 39.5, 5.1 TB/s.
 #include <algorithm>
 
 #include "paged.hpp"
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(AppendArgs a) {
 }
 
 // One workgroup moves the rows of a KV head: all are read before the first is written.  A launch's latency bounds it:
-// 3 rows of 8 heads 2.6 us, 7 rows of 1024 heads 3.5 us.
+// 3 rows of 8 heads 3.4 us, 7 rows of 1024 heads 3.9 us.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void paged_keep_kernel(Paged c, Seqs n, const int32_t* path,
                                                               const int32_t* n_path) {

@@ -17,10 +17,11 @@
 // in LDS, read in the same lanes and order.
 //
 // What bounds it, over 8 heads of 25600 entries of d = 128 in bf16: with 20 rows
-// (5 nodes) memory, 22.4 us and 4.9 TB/s, and 32 such caches in one call
-// 567 us, 6.0 TB/s; with 256 rows (64 nodes) the instructions of the softmax and
-// the matrix cores, which two waves of a SIMD overlap only in part: 69 us, 390
-// TFLOP/s.  The kernel that combines adds 4.6 and 8.9 us.
+// (5 nodes) memory, 23.3 us and 4.7 TB/s, and 32 such caches in one call
+// 569 us, 6.0 TB/s; with 256 rows (64 nodes) the instructions of the softmax and
+// the matrix cores, which two waves of a SIMD overlap only in part: 70 us, 380
+// TFLOP/s.  The kernel that combines adds 4.6 and 8.2 us.  fp32 at d = 128 has
+// registers for one wave a SIMD: 64 nodes 308 us, 87 TFLOP/s, 5 nodes 50 to 57.
 //
 // bf16 weights enter the product as sums of two bf16 numbers (2^-17 of a weight
 // is left; one number, 70 us where two take 79, is 1.4 times as far from 64 bits
@@ -692,7 +693,6 @@ template <typename T, int D, int RT, int RG, int KG>
 __global__ __launch_bounds__(RG * KG * 64, (waves_per_simd<T, D>())) void tree_kernel(TreeArgs a) {
   constexpr int ROWS = 16 * RT;
   constexpr int STEP = KG * kTile;
-  constexpr int RB = D * (int)sizeof(T);
   constexpr int kSlots = KG > 1 ? RG * KG / 2 : 1;
   __shared__ __align__(16) f32x4 s_o[kSlots][KG > 1 ? RT * (D / 16) : 1][64];
   __shared__ float2 s_ml[kSlots][RT][64];
@@ -1072,9 +1072,10 @@ TreePlan plan_rows(int64_t heads, int d, int rows, size_t elem) {
 // the entries of a workgroup, and what one costs besides, times the workgroups of the fullest CU: one layer of 25605
 // entries (8 heads, 5 nodes) takes 27.6 us in 29 splits, one workgroup on most CUs, and 29.2 in 51, two on some; 64
 // nodes 78 in 31 and 101 in 51.  Where lengths are the device's to know, two rounds, and six up to 32 rows, where a
-// workgroup costs less.  Sequences of 0 to 8100 entries, 8 heads: 8 of up to 64 nodes (G 4) take 77 us in two rounds, 92
-// in one and a half and 81 in three; 16 of up to 26 (G 8) 129, 163 and 117; 16 of up to 16 (G 4) 70, 80 and 82; 32 of up
-// to 8 112 in six and 115 in three, 64 of up to one 30 in six and 64 in one and a half.
+// workgroup costs less.  Sequences of 0 to 8100 entries, 8 heads, in one and a half, two, three and four rounds: 8 of up
+// to 64 nodes (G 4) 93, 77, 82 and 90 us; 16 of up to 16 (G 4) 78, 69, 81 and 90; 16 of up to 26 (G 8) 164, 131, 119 and
+// 124: two cost the last 12 us and save the others 5 and 12.  In two, three and six: 32 of up to 8 (G 4) 118, 107 and 112,
+// 64 of up to one 64, 38 and 30.
 TreePlan plan_tree(int64_t heads, int entries, int d, int rows, size_t elem, bool ragged) {
   TreePlan p = plan_rows(heads, d, rows, elem);
   const int64_t units = heads * p.row_blocks;

@@ -17,8 +17,9 @@
 // A sum needs the walk before it, so they take turns: each launch of sum_kernel walks on from what the last one summed
 // (every wave by itself, one node per lane) and sums the next chunk after, over all CUs; draw_kernel, one workgroup a
 // sequence, finishes, by itself where more sums are left than launches, and draws.  What bounds it is that chain: 32
-// trees over 131072 tokens 28.6 us, of them three sums of 5 to 8 and the draw's 7 (one workgroup a sequence for all: 98);
-// one chain of 5 nodes over 32000 tokens 9.7 us.
+// trees over 131072 tokens 28.1 us, of them three sums of 5 to 9 and the draw's 7 (one workgroup a sequence for all: 98),
+// and up to 48 where a tree refuses so often that the draw has sums of its own to take; one chain of 5 nodes over 32000
+// tokens 9.4 us.
 #include <algorithm>
 
 #include "common.hpp"

@@ -647,7 +647,8 @@ def rope_frequencies(rot_dim: int, theta: float, device, scaling: str | None = N
     `device`, and what the rotated part is multiplied by.  For contexts `factor` times as long as those trained on:
     "linear" divides every frequency by it; "ntk" stretches theta so that the lowest one is divided by it and the
     highest stays; "yarn" (arXiv 2309.00071) divides those that turn less than `slow` times within original_len, keeps
-    those that turn more than `fast` times, goes linearly in j between, and multiplies by 0.1 ln(factor) + 1."""
+    those that turn more than `fast` times, goes linearly in j between, and multiplies by 0.1 ln(factor) + 1; as models
+    are trained, the borders of that range are whole pairs, rounded outwards, the upper one rot_dim - 1 at most."""
     if rot_dim < 2 or rot_dim % 2 or not theta > 1.0 or not factor >= 1.0:
         raise ValueError("rot_dim must be even, theta above 1 and factor 1 or more")
     j = torch.arange(rot_dim // 2, dtype=torch.float64)
