@@ -617,8 +617,9 @@ SELKV_API selkv_status selkv_tree_workspace_size(const selkv_params* p, const se
  * root, node i included (their rows as selkv_paged_append stored them).  A bias
  * of -inf masks its entry whatever the entry and the query hold, and no node's
  * row reaches a node that does not attend to it; a node that nothing is left
- * for gives 0.  Any finite bias counts as it is, and means of finite values are
- * finite; an infinite value reaches every node that attends to it, whatever its
+ * for gives 0.  Any finite bias counts as it is.  Means of finite values are
+ * finite (of values beyond 2^96 where a node's largest logit is within 2^24 of
+ * 0); an infinite value reaches every node that attends to it, whatever its
  * weight.  Sums, maxima and logits are fp32; for bf16 the softmax weights enter
  * the product with V as sums of two bf16 numbers.
  * In:  q [B, n, H_kv*G, d] (kv_dtype); parent [B, n] or NULL; 1 <= n <= 64;

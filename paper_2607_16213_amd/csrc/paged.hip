@@ -14,7 +14,7 @@
 // us for 256 heads of 25600 rows, 1213 so; through the caches 1265).  A
 // workgroup's threads go token by token within a head, as pages are laid out.
 //
-// Bound by HBM: 256 heads of 25600 rows (bf16) in 1213 to 1310 us by the box,
+// Bound by HBM: 256 heads of 25600 rows (bf16) in 1213 to 1310 us by the card,
 // 5.2 to 5.6 TB/s read and written, 8191 rows of a prompt with their queries in
 // 39.5, 5.1 TB/s.
 #include <algorithm>

@@ -657,7 +657,7 @@ __device__ __forceinline__ bool all_in_range(const RowTile<D> (&st)[RT]) {
 __device__ __forceinline__ int careful_shift(int end) { return 44 - __clz(end); }
 
 // After a careful pass: rows whose sums are small get the power of two back, which leaves the bits of a pass that never
-// took it off; the others' maximum is raised by as much.
+// took it off; the others' maximum is raised by as much, as nearly as fp32 has it, which up to 2^24 is to 1/2.
 template <int D, int RT>
 __device__ __forceinline__ void settle(RowTile<D> (&st)[RT], int shift) {
 #pragma unroll

@@ -130,6 +130,25 @@ def test_finite_values_give_finite_means(S, dtype, n, G, L, counts, where):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("n,G,L,counts", SHAPES)
+def test_finite_values_under_large_biases(S, dtype, n, G, L, counts):
+    """Means of 3e38 and of 1e38 and 3e38: between them, to the roundings of weights, sums and output."""
+    for value in (-1.6e7, -1e6, -1500.0, 1500.0, 1e6, 1.6e7):
+        c = call(S, dtype, n, G, L, counts, 47)
+        for b in range(len(c.lens)):
+            bias_of(c, b, 0, L + n, value)
+            pg, row = U.places(c.c, b, 0, L + n)
+            c.c.V[pg, :, row] = 3e38
+            c.c.V[pg[::3], :, row[::3], 64:] = 1e38
+        out = c.run()
+        for b in range(len(c.lens)):
+            got = out[b, :c.nodes(b)].double() / 1e38
+            rel = 2.0 ** -7 + (L + n) * 2.0 ** -22
+            assert bool(((got[..., :64] - 3.0).abs() <= 3 * rel).all()), value
+            assert bool((got[..., 64:] <= 3 * (1 + rel)).all()) and bool((got[..., 64:] >= 1 - rel).all()), value
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,G,L,counts", SHAPES)
 def test_infinite_values_with_hardly_a_weight(S, dtype, n, G, L, counts):
     """e^-200 of infinity is infinite, wherever the entry lies: in a row's first tile or its last, in tiles, waves and
     splits of such entries alone or beside others."""
