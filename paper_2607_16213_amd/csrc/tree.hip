@@ -29,10 +29,10 @@
 //
 // Masks.  Entries past the end, on no page or (for a node) outside its chain of
 // parents are left out by selection in the tiles that hold such; a masked bias
-// makes a logit -inf by itself.  Where a result comes out NaN, infinite or past 2^96 the
-// wave does its entries again in a careful pass, in which every tile selects
-// masked biases too, V's values that are NaN or infinite are kept out of the
-// product, where a weight of 0 would turn them into NaN for every row, and are
+// makes a logit -inf by itself.  Where a result comes out NaN, infinite or past
+// 2^96 the wave does its entries again in a careful pass, in which every tile
+// selects masked biases too, V's values that are NaN or infinite are kept out of
+// the product, where a weight of 0 would turn them into NaN for every row, and are
 // added to the rows that attend to them.  Its weights are a power of two smaller,
 // so that no sum of finite values overflows: a mean of finite values is finite.
 //
@@ -403,15 +403,16 @@ __device__ __forceinline__ void logits(float (&p)[RT][8], const Keys<T, D>& x, c
 
 // A row's maximum follows its logits only when they are this far above it, so that after the first tiles of a row hardly a
 // tile has to rescale what is there (one of 32 rows is enough for that: 172 us where 183 without, 16 sequences of 0 to
-// 8100 entries, 26 nodes).  Weights are up to e^6 then, which fp32 sums and the weights' relative rounding do not mind.
+// 8100 entries, 26 nodes).  Weights are up to e^6 then, which their relative rounding does not mind, nor do fp32 sums up to
+// kRoom.
 constexpr float kSlack = 6.f;
 
-// Logits to weights, with the running maximum and sum; the weights are multiplied by `lower`.  Before bf16 weights the maximum is taken off by the fma that
-// turns a logit to powers of two.  Its product with log2(e) is rounded once, the same for all of a row, so weights are off
-// by one factor: up to |m| = kFar by 2^-14 of themselves at most, as much as a logit's own rounding moves it.  The factor
-// grows with |m| (up to 2^64 at 1e9, out of any range at 1e11), so a row with a maximum beyond kFar has it taken off first.
+// A bf16 row whose maximum is beyond this has it taken off its logits before the fma that turns them to powers of two.  The
+// fma takes off the maximum times log2(e), rounded, so it puts one factor on all weights of a row: up to here within 2^-14
+// of 1, as much as a logit's own rounding; 2^64 or its inverse at 1e9, out of any range at 1e11.
 constexpr float kFar = 1024.f;
 
+// Logits to weights, with the running maximum and sum; the weights are multiplied by `lower`.
 template <bool FUSED, int D, int RT>
 __device__ __forceinline__ void soften(RowTile<D> (&st)[RT], float (&p)[RT][8], float lower) {
   float top[RT];
